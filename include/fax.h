@@ -422,6 +422,88 @@ int fax_cross_entropy_static(int dtype, int N, int V, const void* logits, const 
 int fax_cross_entropy_static_max_rows(void);
 
 /*
+ * The way into a model and its gradient, for programs that drive their own layers.
+ * tokens: int32 [N] on the device.  An id outside [0, V) stands for no token (padding): its row of the output is zero, and it
+ * adds nothing to the gradient.  Arithmetic in fp32, one rounding to dtype.
+ *   fax_embedding_fwd:  out[n] = scale table[tokens[n]];  table [V, D], out [N, D] in dtype.
+ *   fax_embedding_bwd:  dtable[v] (+)= scale (sum of dout[n] over the positions n that hold id v);  dout [N, D] in dtype, dtable fp32
+ *     [V, D].  accumulate = 0 overwrites every row (with zero where no position holds the id), otherwise the sums are added and rows
+ *     without a position are left as they are.  Positions are sorted by id first, every row has one writer, and its terms are
+ *     added in an order that depends on the tokens alone: the same call gives the same bits.
+ *     ws: fax_embedding_bwd_workspace_bytes().
+ * N = 0 is no error (the gradient without accumulate is then zero).
+ */
+int fax_embedding_fwd(int dtype, int N, int V, int D, const int32_t* tokens, const void* table, float scale, void* out, void* stream);
+int fax_embedding_bwd_workspace_bytes(int N, int V, int D, size_t* out);
+int fax_embedding_bwd(int dtype, int N, int V, int D, const int32_t* tokens, const void* dout, float scale, float* dtable, int accumulate,
+                      void* ws, size_t ws_bytes, void* stream);
+
+/*
+ * Causal attention in a sliding window, with the first keys (sinks) always in sight, and with key heads that several query heads
+ * share: local layers of long-context models; whole sequences for training, chunks of prompts and single tokens over a cache.
+ *   Query i of sequence b stands at position p = q_pos[b] + i.  Key j is visible to it where
+ *     j < k_len[b]  and  j <= p  and  (j > p - window  or  j < sinks).
+ *   s_ij = q_i . k_j / sqrt(dh);  ctx_i = sum_j softmax_j(s_ij) v_j;  lse_i = log sum_j e^(s_ij).
+ *   A query that sees no key has ctx = 0, lse = -infinity and no gradient.
+ *   Query head h reads key head h / (H / Hkv).  q, dq: [B, Sq, H, dh]; k, v, dk, dv: [B, Sk, Hkv, dh]; ctx, dctx: [B, Sq, H, dh]
+ *   in dims.dtype; lse: fp32 [B, H, Sq].
+ * Strides say, in elements, how far apart sequences, rows and heads are (features are adjacent): views into a packed
+ *   projection, or a cache with heads outside of rows.  A FaxStrides of three zeros means stored densely in the order above.  dims.q holds for q and
+ *   dq, dims.kv for k, v, dk, dv, dims.ctx for ctx and dctx.  Elements of an output may not overlap.
+ * q_pos, k_len: int32 [B] on the device.  q_pos NULL: the queries are the last Sq of Sk positions (q_pos = Sk - Sq: 0 for a whole
+ *   sequence, the newest token for Sq = 1).  k_len NULL: Sk.  k_len counts as 0 below zero and as Sk above; q_pos as -2^30 below that and as
+ *   2^30 - Sq above that.  Rows of k and v from k_len on are not used, whatever they hold, and get zeros in dk and dv.
+ * Sizes up to B * max(Sq, Sk) = 2^30, dh <= 256, window >= 1, sinks >= 0; H a multiple of Hkv.
+ * q, k, v, ctx and their gradients may start at any element (not the 16-byte alignment of the other calls): rows that start on 16 bytes take the
+ *   matrix cores where the head width is a multiple of 16 bytes and at most 128 (fax_window_attention_route tells), others scalar kernels.
+ * lse may be NULL in the forward pass (inference).  Backward: ctx, lse as the forward pass left them; dq, dk, dv are overwritten.
+ * ws: fax_window_attention_workspace_bytes(), which covers both passes.  Nothing in it is kept from call to call.
+ * No atomics: two calls on the same inputs give the same bits.
+ */
+typedef struct FaxStrides {
+  int64_t batch, row, head;
+} FaxStrides;
+typedef struct FaxWindowDims {
+  int32_t B, Sq, Sk, H, Hkv, dh;
+  int32_t dtype; /* FAX_F32 | FAX_BF16 */
+  int32_t window, sinks;
+  FaxStrides q, kv, ctx;
+} FaxWindowDims;
+int fax_window_attention_workspace_bytes(const FaxWindowDims* dims, size_t* out);
+int fax_window_attention_fwd(const FaxWindowDims* dims, const void* q, const void* k, const void* v, const int32_t* q_pos,
+                             const int32_t* k_len, void* ctx, float* lse, void* ws, size_t ws_bytes, void* stream);
+int fax_window_attention_bwd(const FaxWindowDims* dims, const void* q, const void* k, const void* v, const int32_t* q_pos,
+                             const int32_t* k_len, const void* ctx, const float* lse, const void* dctx, void* dq, void* dk, void* dv,
+                             void* ws, size_t ws_bytes, void* stream);
+
+/*
+ * AdamW (as fax_adamw_step) on any number of tensors, with moments of 32 or of 8 bits.
+ * tensors: HOST array.  master, grad, lowp, n as in fax_adamw_step (lowp NULL to skip); decay = 0: this tensor takes no weight decay.
+ *   Tensors may not overlap.  n = 0 is skipped.
+ * state FAX_STATE_F32: m, v fp32 [n]; m_scale, v_scale unused.
+ * state FAX_STATE_E4M3: m, v one byte an element, 8-bit floating-point numbers (four exponent, three mantissa bits, largest 448), and a scale
+ *   for every 256 consecutive elements: m_scale, v_scale fp32 [(n + 255) / 256], 4-byte aligned.  The first moment is m m_scale, the second
+ *   (v v_scale)^2.  Zero bytes and scales are the state before the first step.  The update itself uses the new moments before they are
+ *   rounded.  m is rounded to nearest.  The root of the second moment is rounded up or down at random, so that its mean is kept: it moves by less than
+ *   a thousandth of itself a step, which no nearest rounding to steps of a sixteenth would ever pass on.  What is not zero stays at least the smallest
+ *   number that is not (2^-9 of a scale), as it divides.  A block whose first moments are all below 2^-100 keeps zeros.  An element whose gradient is
+ *   infinite or NaN loses its own state (NaN), not its block's.
+ *   The random bits of element i of tensors[t] are those of i, t, step and `seed`: h(h(seed + step c) + t c) =: key, h(i c + key) >> 12
+ *   with c = 0x9E3779B1 and h(x): x ^= x >> 16; x *= c; x ^= x >> 15; x *= 0x2545F491; x ^= x >> 16, all modulo 2^32.
+ */
+enum { FAX_STATE_F32 = 0, FAX_STATE_E4M3 = 1 };
+typedef struct FaxAdamWTensor {
+  void *master, *m, *v;
+  const void* grad;
+  void* lowp;
+  float *m_scale, *v_scale;
+  size_t n;
+  int32_t grad_dtype; /* FAX_F32 | FAX_BF16 */
+  int32_t decay;
+} FaxAdamWTensor;
+int fax_adamw_multi_step(int state, int count, const FaxAdamWTensor* tensors, const FaxAdamW* hp, int step, uint32_t seed, void* stream);
+
+/*
  * Measured ceilings, for benchmarks: what this GPU delivers to a kernel that does nothing but
  * matrix-core instructions, and to one that does nothing but copy.  Timed like every other kernel
  * through fax_timing_enable / fax_timing_report (rows "probe_mfma_zero", "probe_mfma_random",

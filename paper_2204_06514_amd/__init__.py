@@ -23,6 +23,7 @@ FAX_FLAG_SINGLE_STREAM = 2
 FAX_FLAG_SKIP_UPDATE = 1
 FAX_FLAG_ACCUMULATE = 2
 FAX_FLAG_DETERMINISTIC = 4
+FAX_STATE_F32, FAX_STATE_E4M3 = 0, 1
 PATH_AUTO, PATH_SCALAR, PATH_MFMA = 0, 1, 2
 FAX_GEMM_SCALAR, FAX_GEMM_F32, FAX_GEMM_MFMA, FAX_GEMM_EDGE, FAX_GEMM_SMALL = 0, 1, 2, 3, 4
 FAX_ATTENTION_SCALAR, FAX_ATTENTION_F32, FAX_ATTENTION_MFMA, FAX_ATTENTION_EDGE = 0, 1, 2, 3
@@ -81,6 +82,20 @@ class FaxAttentionRoute(C.Structure):
     _fields_ = [(n, C.c_int32) for n in ("form", "groups", "waves", "bwd_groups", "bwd_waves", "joint")]
 
 
+class FaxStrides(C.Structure):
+    _fields_ = [(n, C.c_int64) for n in ("batch", "row", "head")]
+
+
+class FaxWindowDims(C.Structure):
+    _fields_ = [(n, C.c_int32) for n in ("B", "Sq", "Sk", "H", "Hkv", "dh", "dtype", "window", "sinks")] + [
+        (n, FaxStrides) for n in ("q", "kv", "ctx")]
+
+
+class FaxAdamWTensor(C.Structure):
+    _fields_ = [(n, C.c_void_p) for n in ("master", "m", "v", "grad", "lowp", "m_scale", "v_scale")] + [
+        ("n", C.c_size_t), ("grad_dtype", C.c_int32), ("decay", C.c_int32)]
+
+
 class FaxMesh(C.Structure):
     _fields_ = [("data", C.c_int32), ("tensor", C.c_int32)]
 
@@ -136,6 +151,13 @@ def _load():
         "fax_cross_entropy": (i32, [i32, i32, i32, vp, vp, vp, vp, vp, vp]),
         "fax_cross_entropy_static": (i32, [i32, i32, i32, vp, vp, vp, vp, vp]),
         "fax_cross_entropy_static_max_rows": (i32, []),
+        "fax_embedding_fwd": (i32, [i32] * 4 + [vp, vp, f32, vp, vp]),
+        "fax_embedding_bwd_workspace_bytes": (i32, [i32] * 3 + [P(sz)]),
+        "fax_embedding_bwd": (i32, [i32] * 4 + [vp, vp, f32, vp, i32, vp, sz, vp]),
+        "fax_window_attention_workspace_bytes": (i32, [P(FaxWindowDims), P(sz)]),
+        "fax_window_attention_fwd": (i32, [P(FaxWindowDims)] + [vp] * 8 + [sz, vp]),
+        "fax_window_attention_bwd": (i32, [P(FaxWindowDims)] + [vp] * 12 + [sz, vp]),
+        "fax_adamw_multi_step": (i32, [i32, i32, P(FaxAdamWTensor), P(FaxAdamW), i32, C.c_uint32, vp]),
         "fax_probe_mfma": (i32, [i32, i32, C.c_uint, vp, vp]),
         "fax_probe_copy": (i32, [vp, vp, sz, vp]),
         "fax_analyze": (i32, [P(FaxModelDims), P(FaxMesh), P(FaxAnalysis)]),
@@ -360,6 +382,88 @@ def fax_attention_route(dtype, B, S, H, dh):
     out = FaxAttentionRoute()
     _check(_lib.fax_attention_route(dtype, B, S, H, dh, C.byref(out)))
     return out
+
+
+def fax_embedding_fwd(dtype, N, V, D, tokens, table, scale, out, stream=None):
+    _check(_lib.fax_embedding_fwd(dtype, N, V, D, _ptr(tokens), _ptr(table), scale, _ptr(out), _stream(stream)))
+
+
+def fax_embedding_bwd_workspace_bytes(N, V, D):
+    out = C.c_size_t()
+    _check(_lib.fax_embedding_bwd_workspace_bytes(N, V, D, C.byref(out)))
+    return out.value
+
+
+def fax_embedding_bwd(dtype, N, V, D, tokens, dout, scale, dtable, accumulate, ws, ws_bytes, stream=None):
+    _check(_lib.fax_embedding_bwd(dtype, N, V, D, _ptr(tokens), _ptr(dout), scale, _ptr(dtable), int(accumulate), _ptr(ws),
+                                  ws_bytes, _stream(stream)))
+
+
+def _strides(t):
+    """[B, S, heads, dh] -> FaxStrides; dimensions of one element have no stride."""
+    assert t.dim() == 4 and (t.stride(3) == 1 or t.size(3) == 1), "features have to be adjacent"
+    return FaxStrides(*t.stride()[:3])
+
+
+def window_dims(q, k, window, sinks=0, ctx=None):
+    """Sizes and strides of q [B, Sq, H, dh] (dq alike) and k [B, Sk, Hkv, dh] (v, dk, dv alike), views into something larger or not;
+    ctx: [B, Sq, H, dh] if not stored densely."""
+    B, Sq, H, dh = q.shape
+    assert k.size(0) == B and k.size(3) == dh and k.dtype == q.dtype, "q and k differ in batch, head width or type"
+    assert ctx is None or ctx.shape == q.shape, "ctx has the shape of q"
+    return FaxWindowDims(B, Sq, k.size(1), H, k.size(2), dh, dtype_code(q), window, sinks, _strides(q), _strides(k),
+                         _strides(ctx) if ctx is not None else FaxStrides(0, 0, 0))
+
+
+def _laid_out(t, dims, name, strides):
+    """Address of a tensor that is laid out as `dims` says (an address is taken as it is)."""
+    if t is None or isinstance(t, int):
+        return t
+    rows, heads = (dims.Sk, dims.Hkv) if name == "kv" else (dims.Sq, dims.H)
+    shape = (dims.B, rows, heads, dims.dh)
+    s = (strides.batch, strides.row, strides.head)
+    if s == (0, 0, 0):
+        s = (rows * heads * dims.dh, heads * dims.dh, dims.dh)
+    assert t.shape == shape, "a tensor of %s where dims say %s" % (tuple(t.shape), shape)
+    assert all(n == 1 or x == y for n, x, y in zip(shape, t.stride(), s + (1,))), "strides %s where dims.%s says %s" % (t.stride(), name, s)
+    return t.data_ptr()
+
+
+def fax_window_attention_workspace_bytes(dims):
+    out = C.c_size_t()
+    _check(_lib.fax_window_attention_workspace_bytes(C.byref(dims), C.byref(out)))
+    return out.value
+
+
+def fax_window_attention_fwd(dims, q, k, v, q_pos, k_len, ctx, lse, ws, ws_bytes, stream=None):
+    """q, k, v, ctx: laid out as `dims` says."""
+    at = lambda t, name: _laid_out(t, dims, name, getattr(dims, name))  # noqa: E731
+    _check(_lib.fax_window_attention_fwd(C.byref(dims), at(q, "q"), at(k, "kv"), at(v, "kv"), _ptr(q_pos), _ptr(k_len), at(ctx, "ctx"),
+                                         _ptr(lse), _ptr(ws), ws_bytes, _stream(stream)))
+
+
+def fax_window_attention_bwd(dims, q, k, v, q_pos, k_len, ctx, lse, dctx, dq, dk, dv, ws, ws_bytes, stream=None):
+    at = lambda t, name: _laid_out(t, dims, name, getattr(dims, name))  # noqa: E731
+    _check(_lib.fax_window_attention_bwd(C.byref(dims), at(q, "q"), at(k, "kv"), at(v, "kv"), _ptr(q_pos), _ptr(k_len), at(ctx, "ctx"),
+                                         _ptr(lse), at(dctx, "ctx"), at(dq, "q"), at(dk, "kv"), at(dv, "kv"), _ptr(ws), ws_bytes,
+                                         _stream(stream)))
+
+
+def adamw_tensors(tensors):
+    """[{master, m, v, grad, lowp, m_scale, v_scale, decay}, ...] (lowp, the scales and decay may be left out) -> the host array for
+    fax_adamw_multi_step.  It holds addresses: the tensors have to live as long as it is used."""
+    arr = (FaxAdamWTensor * max(len(tensors), 1))()
+    for e, t in zip(arr, tensors):
+        for n in ("master", "m", "v", "grad", "lowp", "m_scale", "v_scale"):
+            setattr(e, n, _ptr(t.get(n)))
+        e.n, e.grad_dtype, e.decay = t["master"].numel(), dtype_code(t["grad"]), int(t.get("decay", True))
+    return arr, len(tensors)
+
+
+def fax_adamw_multi_step(state, tensors, hp, step, seed=0, stream=None):
+    """tensors: of adamw_tensors."""
+    arr, count = tensors
+    _check(_lib.fax_adamw_multi_step(state, count, arr, C.byref(hp) if hp is not None else None, step, seed, _stream(stream)))
 
 
 def fax_timing_enable(on):

@@ -7,6 +7,7 @@
 #include <map>
 #include <mutex>
 #include <string>
+#include <utility>
 #include <vector>
 
 #include "fax_internal.h"
@@ -1103,6 +1104,177 @@ int fax_cross_entropy(int dtype, int N, int V, const void* logits, const int32_t
   FAX_TRY(check_ptr(logits, "logits")); FAX_TRY(check_ptr(labels, "labels")); FAX_TRY(check_ptr(dlogits, "dlogits"));
   FAX_TRY(check_ptr(row_loss, "row_loss")); FAX_TRY(check_ptr(loss_out, "loss_out"));
   return cross_entropy(dtype, N, V, V, logits, labels, dlogits, row_loss, loss_out, 1.0f, (hipStream_t)stream);
+}
+
+static int check_embedding(int dtype, int N, int V, int D) {
+  if (dtype != FAX_F32 && dtype != FAX_BF16) { set_error("bad dtype %d", dtype); return FAX_ERR_INVALID_ARG; }
+  if (N < 0 || V <= 0 || D <= 0) { set_error("bad embedding size N=%d V=%d D=%d", N, V, D); return FAX_ERR_INVALID_ARG; }
+  if (N > (1 << 30) || V > (1 << 30) || D > (1 << 24)) { set_error("embedding: N or V exceeds 2^30, or D 2^24"); return FAX_ERR_UNSUPPORTED; }
+  return FAX_OK;
+}
+
+int fax_embedding_fwd(int dtype, int N, int V, int D, const int32_t* tokens, const void* table, float scale, void* out, void* stream) {
+  FAX_TRY(check_embedding(dtype, N, V, D));
+  if (N == 0) return FAX_OK;
+  FAX_TRY(check_ptr(tokens, "tokens")); FAX_TRY(check_ptr(table, "table")); FAX_TRY(check_ptr(out, "out"));
+  return embedding_fwd(dtype, N, V, D, tokens, table, scale, out, (hipStream_t)stream);
+}
+
+int fax_embedding_bwd_workspace_bytes(int N, int V, int D, size_t* out) {
+  FAX_TRY(check_embedding(FAX_F32, N, V, D));
+  if (!out) { set_error("out is NULL"); return FAX_ERR_INVALID_ARG; }
+  *out = embedding_bwd_ws_bytes(N, V, D);
+  return FAX_OK;
+}
+
+int fax_embedding_bwd(int dtype, int N, int V, int D, const int32_t* tokens, const void* dout, float scale, float* dtable, int accumulate,
+                      void* ws, size_t ws_bytes, void* stream) {
+  FAX_TRY(check_embedding(dtype, N, V, D));
+  FAX_TRY(check_ptr(dtable, "dtable"));
+  if (N > 0) {
+    FAX_TRY(check_ptr(tokens, "tokens")); FAX_TRY(check_ptr(dout, "dout")); FAX_TRY(check_ptr(ws, "ws"));
+    const size_t need = embedding_bwd_ws_bytes(N, V, D);
+    if (ws_bytes < need) { set_error("workspace of %zu bytes is smaller than the %zu required", ws_bytes, need); return FAX_ERR_WORKSPACE; }
+  }
+  return embedding_bwd(dtype, N, V, D, tokens, dout, scale, dtable, accumulate != 0, ws, (hipStream_t)stream);
+}
+
+static int fill_strides(FaxStrides* s, const char* name, int S, int heads, int dh) {
+  if (s->batch == 0 && s->row == 0 && s->head == 0) {
+    s->head = dh;
+    s->row = (int64_t)heads * dh;
+    s->batch = (int64_t)S * heads * dh;
+    return FAX_OK;
+  }
+  if (s->batch < 0 || s->row < 0 || s->head < 0) { set_error("%s: negative stride", name); return FAX_ERR_INVALID_ARG; }
+  return FAX_OK;
+}
+
+// Whether two elements share a place, as far as strides that are sorted and nested tell: every one clears the extent of the smaller ones.
+static bool overlapping(const FaxStrides& s, int B, int S, int heads, int dh) {
+  int64_t st[3] = {s.batch, s.row, s.head}, n[3] = {B, S, heads};
+  for (int i = 0; i < 3; i++)
+    for (int j = i + 1; j < 3; j++)
+      if (st[j] < st[i]) { std::swap(st[i], st[j]); std::swap(n[i], n[j]); }
+  int64_t extent = dh;
+  for (int i = 0; i < 3; i++) {
+    if (n[i] == 1) continue;
+    if (st[i] < extent) return true;
+    if (st[i] > (int64_t)1 << 40) return false;  // beyond any memory: refused by the caller's check
+    extent += st[i] * (n[i] - 1);
+  }
+  return false;
+}
+
+// Checks `dims` and returns a copy with strides filled in.
+static int check_window(const FaxWindowDims* dims, FaxWindowDims* out) {
+  if (!dims) { set_error("dims is NULL"); return FAX_ERR_INVALID_ARG; }
+  FaxWindowDims d = *dims;
+  if (d.dtype != FAX_F32 && d.dtype != FAX_BF16) { set_error("dtype %d is neither FAX_F32 nor FAX_BF16", d.dtype); return FAX_ERR_INVALID_ARG; }
+  if (d.B <= 0 || d.Sq <= 0 || d.Sk <= 0 || d.H <= 0 || d.Hkv <= 0 || d.dh <= 0) {
+    set_error("non-positive dimension: B=%d Sq=%d Sk=%d H=%d Hkv=%d dh=%d", d.B, d.Sq, d.Sk, d.H, d.Hkv, d.dh);
+    return FAX_ERR_INVALID_ARG;
+  }
+  if (d.H % d.Hkv) { set_error("H=%d is no multiple of Hkv=%d", d.H, d.Hkv); return FAX_ERR_INVALID_ARG; }
+  if (d.window < 1 || d.sinks < 0) { set_error("window=%d must be >= 1, sinks=%d >= 0", d.window, d.sinks); return FAX_ERR_INVALID_ARG; }
+  if (d.dh > 256) { set_error("head width %d exceeds 256", d.dh); return FAX_ERR_UNSUPPORTED; }
+  const int64_t most = (int64_t)1 << 30;
+  if ((int64_t)d.B * d.Sq > most || (int64_t)d.B * d.Sk > most || (int64_t)d.B * d.Sq * d.H > 4 * most || (int64_t)d.B * d.Sk * d.Hkv > 4 * most) {
+    set_error("B*Sq or B*Sk exceeds 2^30, or with the heads 2^32");
+    return FAX_ERR_UNSUPPORTED;
+  }
+  FAX_TRY(fill_strides(&d.q, "dims.q", d.Sq, d.H, d.dh));
+  FAX_TRY(fill_strides(&d.kv, "dims.kv", d.Sk, d.Hkv, d.dh));
+  FAX_TRY(fill_strides(&d.ctx, "dims.ctx", d.Sq, d.H, d.dh));
+  for (const FaxStrides* s : {&d.q, &d.kv, &d.ctx})
+    if (s->batch > (int64_t)1 << 40 || s->row > (int64_t)1 << 40 || s->head > (int64_t)1 << 40) {
+      set_error("a stride exceeds 2^40 elements");
+      return FAX_ERR_UNSUPPORTED;
+    }
+  if (overlapping(d.ctx, d.B, d.Sq, d.H, d.dh)) { set_error("dims.ctx: elements overlap"); return FAX_ERR_INVALID_ARG; }
+  *out = d;
+  return FAX_OK;
+}
+
+static int check_elements(const void* p, int dtype, const char* name) {
+  if (!p) { set_error("%s is NULL", name); return FAX_ERR_INVALID_ARG; }
+  if (reinterpret_cast<uintptr_t>(p) % esize(dtype)) { set_error("%s is not aligned to its elements", name); return FAX_ERR_INVALID_ARG; }
+  return FAX_OK;
+}
+static int check_ints(const int32_t* p, const char* name) {
+  if (reinterpret_cast<uintptr_t>(p) % 4) { set_error("%s is not aligned to its elements", name); return FAX_ERR_INVALID_ARG; }
+  return FAX_OK;
+}
+
+int fax_window_attention_workspace_bytes(const FaxWindowDims* dims, size_t* out) {
+  FaxWindowDims d;
+  FAX_TRY(check_window(dims, &d));
+  if (!out) { set_error("out is NULL"); return FAX_ERR_INVALID_ARG; }
+  *out = window_ws_bytes(d);
+  return FAX_OK;
+}
+
+static int check_window_ws(const FaxWindowDims& d, const void* ws, size_t ws_bytes) {
+  FAX_TRY(check_ptr(ws, "ws"));
+  const size_t need = window_ws_bytes(d);
+  if (ws_bytes < need) { set_error("workspace of %zu bytes is smaller than the %zu required", ws_bytes, need); return FAX_ERR_WORKSPACE; }
+  return FAX_OK;
+}
+
+int fax_window_attention_fwd(const FaxWindowDims* dims, const void* q, const void* k, const void* v, const int32_t* q_pos,
+                             const int32_t* k_len, void* ctx, float* lse, void* ws, size_t ws_bytes, void* stream) {
+  FaxWindowDims d;
+  FAX_TRY(check_window(dims, &d));
+  FAX_TRY(check_elements(q, d.dtype, "q")); FAX_TRY(check_elements(k, d.dtype, "k")); FAX_TRY(check_elements(v, d.dtype, "v"));
+  FAX_TRY(check_elements(ctx, d.dtype, "ctx"));
+  FAX_TRY(check_ints(q_pos, "q_pos")); FAX_TRY(check_ints(k_len, "k_len"));
+  if (lse) FAX_TRY(check_elements(lse, FAX_F32, "lse"));
+  FAX_TRY(check_window_ws(d, ws, ws_bytes));
+  return window_fwd(d, q, k, v, q_pos, k_len, ctx, lse, ws, (hipStream_t)stream);
+}
+
+int fax_window_attention_bwd(const FaxWindowDims* dims, const void* q, const void* k, const void* v, const int32_t* q_pos,
+                             const int32_t* k_len, const void* ctx, const float* lse, const void* dctx, void* dq, void* dk, void* dv,
+                             void* ws, size_t ws_bytes, void* stream) {
+  FaxWindowDims d;
+  FAX_TRY(check_window(dims, &d));
+  if (overlapping(d.q, d.B, d.Sq, d.H, d.dh)) { set_error("dims.q: elements of dq overlap"); return FAX_ERR_INVALID_ARG; }
+  if (overlapping(d.kv, d.B, d.Sk, d.Hkv, d.dh)) { set_error("dims.kv: elements of dk, dv overlap"); return FAX_ERR_INVALID_ARG; }
+  const void* const p[8] = {q, k, v, ctx, dctx, dq, dk, dv};
+  const char* const names[8] = {"q", "k", "v", "ctx", "dctx", "dq", "dk", "dv"};
+  for (int i = 0; i < 8; i++) FAX_TRY(check_elements(p[i], d.dtype, names[i]));
+  FAX_TRY(check_elements(lse, FAX_F32, "lse"));
+  FAX_TRY(check_ints(q_pos, "q_pos")); FAX_TRY(check_ints(k_len, "k_len"));
+  FAX_TRY(check_window_ws(d, ws, ws_bytes));
+  return window_bwd(d, q, k, v, q_pos, k_len, ctx, lse, dctx, dq, dk, dv, ws, (hipStream_t)stream);
+}
+
+int fax_adamw_multi_step(int state, int count, const FaxAdamWTensor* tensors, const FaxAdamW* hp, int step, uint32_t seed, void* stream) {
+  if (state != FAX_STATE_F32 && state != FAX_STATE_E4M3) { set_error("state %d is neither FAX_STATE_F32 nor FAX_STATE_E4M3", state); return FAX_ERR_INVALID_ARG; }
+  if (count < 0) { set_error("negative count"); return FAX_ERR_INVALID_ARG; }
+  if (count > 0 && !tensors) { set_error("tensors is NULL"); return FAX_ERR_INVALID_ARG; }
+  FAX_TRY(check_adamw(hp, step));
+  for (int i = 0; i < count; i++) {
+    const FaxAdamWTensor& t = tensors[i];
+    if (t.n == 0) continue;
+    const void* const p[4] = {t.master, t.m, t.v, t.grad};
+    const char* const names[4] = {"master", "m", "v", "grad"};
+    for (int k = 0; k < 4; k++) {
+      if (!p[k]) { set_error("tensors[%d].%s is NULL", i, names[k]); return FAX_ERR_INVALID_ARG; }
+      if (misaligned(p[k])) { set_error("tensors[%d].%s is not 16-byte aligned", i, names[k]); return FAX_ERR_INVALID_ARG; }
+    }
+    if (t.lowp && misaligned(t.lowp)) { set_error("tensors[%d].lowp is not 16-byte aligned", i); return FAX_ERR_INVALID_ARG; }
+    if (t.grad_dtype != FAX_F32 && t.grad_dtype != FAX_BF16) { set_error("tensors[%d].grad_dtype must be FAX_F32 or FAX_BF16", i); return FAX_ERR_INVALID_ARG; }
+    if (t.n > (size_t)1 << 42) { set_error("tensors[%d]: %zu elements", i, t.n); return FAX_ERR_UNSUPPORTED; }
+    if (state == FAX_STATE_E4M3) {
+      if (!t.m_scale || !t.v_scale) { set_error("tensors[%d]: m_scale or v_scale is NULL", i); return FAX_ERR_INVALID_ARG; }
+      if ((reinterpret_cast<uintptr_t>(t.m_scale) | reinterpret_cast<uintptr_t>(t.v_scale)) & 3) {
+        set_error("tensors[%d]: m_scale or v_scale is not aligned to its elements", i);
+        return FAX_ERR_INVALID_ARG;
+      }
+    }
+  }
+  return adamw_multi(state, count, tensors, *hp, step, seed, (hipStream_t)stream);
 }
 
 int fax_probe_mfma(int workgroups, int iters, unsigned seed, float* sink, void* stream) {

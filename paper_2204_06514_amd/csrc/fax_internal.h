@@ -258,6 +258,20 @@ struct AdamWQueue {
 int adamw(float* master, float* m, float* v, const void* grad, int grad_dtype, void* lowp, size_t n, const FaxAdamW& hp,
           int step, hipStream_t s);
 int fill_zero(void* p, size_t bytes, hipStream_t s);
+// tensors: checked, any number (kernels_adamw_multi.hip)
+int adamw_multi(int state, int count, const FaxAdamWTensor* tensors, const FaxAdamW& hp, int step, uint32_t seed, hipStream_t s);
+// Lookup and gradient by themselves (kernels_embedding.hip): ids outside [0, V) are padding.
+int embedding_fwd(int dtype, int N, int V, int D, const int32_t* tokens, const void* table, float scale, void* out, hipStream_t s);
+size_t embedding_bwd_ws_bytes(int N, int V, int D);
+int embedding_bwd(int dtype, int N, int V, int D, const int32_t* tokens, const void* dout, float scale, float* dtable, bool accumulate, void* ws,
+                  hipStream_t s);
+
+// ---- attention in a window (dims checked, with their strides filled in) ----------------------------
+size_t window_ws_bytes(const FaxWindowDims& d);
+int window_fwd(const FaxWindowDims& d, const void* q, const void* k, const void* v, const int32_t* q_pos, const int32_t* k_len, void* ctx,
+               float* lse, void* ws, hipStream_t s);
+int window_bwd(const FaxWindowDims& d, const void* q, const void* k, const void* v, const int32_t* q_pos, const int32_t* k_len, const void* ctx,
+               const float* lse, const void* dctx, void* dq, void* dk, void* dv, void* ws, hipStream_t s);
 
 // ---- measured ceilings (probes.hip) ---------------------------------------------------------------
 int probe_mfma(int workgroups, int iters, unsigned seed, float* sink, hipStream_t s);

@@ -2,7 +2,7 @@
 // over the logits), embedding gather / scatter, and the AdamW update.
 #include <mutex>
 
-#include "fax_internal.h"
+#include "adamw.h"
 
 namespace fax {
 
@@ -469,22 +469,6 @@ int embed_bwd(int dtype, int B, int S, int D, int V, const int32_t* tokens, cons
 // ---------------------------------------------------------------------------------------------
 // AdamW: 16 B/param read (g, p, m, v) + 12 B/param written (+2 for the bf16 copy).
 // ---------------------------------------------------------------------------------------------
-// Streaming stores for values this kernel does not read again.
-__device__ __forceinline__ void nt_store4(float4* p, float4 v) {
-  typedef __attribute__((ext_vector_type(4))) float f4;
-  const f4 x = {v.x, v.y, v.z, v.w};
-  __builtin_nontemporal_store(x, reinterpret_cast<f4*>(p));
-}
-__device__ __forceinline__ void nt_store2(uint2* p, uint2 v) {
-  typedef __attribute__((ext_vector_type(2))) unsigned u2;
-  const u2 x = {v.x, v.y};
-  __builtin_nontemporal_store(x, reinterpret_cast<u2*>(p));
-}
-
-struct AdamScalars {
-  float b1, b2, one_m_b1, one_m_b2, inv_bc1, inv_bc2, lr, eps, decay;
-};
-
 __device__ __forceinline__ void adam_one(float g, float& p, float& m, float& v, const AdamScalars& a) {
   m = a.b1 * m + a.one_m_b1 * g;
   v = a.b2 * v + a.one_m_b2 * g * g;
@@ -532,8 +516,6 @@ __global__ __launch_bounds__(256) void adamw_kernel(size_t n, float* __restrict_
     if (lowp) lowp[i] = (bf16_t)pp;
   }
 }
-
-static AdamScalars adam_scalars(const FaxAdamW& hp, int step);
 
 int adamw(float* master, float* m, float* v, const void* grad, int grad_dtype, void* lowp, size_t n, const FaxAdamW& hp,
           int step, hipStream_t s) {
@@ -595,17 +577,6 @@ __global__ __launch_bounds__(256) void adamw_multi_kernel(AdamWBatch b, AdamScal
     p[i] = pp; m[i] = mm; v[i] = vv;
     if (lowp) lowp[i] = (bf16_t)pp;
   }
-}
-
-static AdamScalars adam_scalars(const FaxAdamW& hp, int step) {
-  AdamScalars a;
-  a.b1 = (float)hp.beta1; a.b2 = (float)hp.beta2;
-  a.one_m_b1 = (float)(1.0 - hp.beta1); a.one_m_b2 = (float)(1.0 - hp.beta2);
-  a.inv_bc1 = (float)(1.0 / (1.0 - pow(hp.beta1, (double)step)));
-  a.inv_bc2 = (float)(1.0 / (1.0 - pow(hp.beta2, (double)step)));
-  a.lr = (float)hp.lr; a.eps = (float)hp.eps;
-  a.decay = (float)(1.0 - hp.lr * hp.wd);
-  return a;
 }
 
 int AdamWQueue::add(float* master, float* m, float* v, const float* grad, void* lowp, size_t n) {

@@ -1,0 +1,91 @@
+// Attention in a sliding window with sinks: the scalar kernels, one wavefront to a row, for any head width up to 256 and any
+// alignment, and the choice between them and the matrix-core kernels.
+#include "attn_window.h"
+
+namespace fax {
+
+static constexpr int MAX_R = 4;  // 64-wide pieces of a head width of 256
+
+// Rows in the order (sequence, query, head) or (sequence, key, key head): neighbours share what they stream.
+template <typename T, int WHAT>  // 0 forward, 1 dQ, 2 dK and dV, 3 delta
+__global__ __launch_bounds__(256) void window_rows_kernel(WindowArgs a) {
+  const int lane = threadIdx.x & 63;
+  const int heads = WHAT == 2 ? a.Hkv : a.H, S = WHAT == 2 ? a.Sk : a.Sq;
+  const long long row = (long long)blockIdx.x * 4 + (threadIdx.x >> 6), rows = (long long)a.B * S * heads;
+  if (row >= rows) return;
+  const int h = (int)(row % heads), i = (int)(row / heads % S), b = (int)(row / heads / S);
+  if constexpr (WHAT == 0) window_fwd_row<MAX_R, T>(a, b, i, h, lane);
+  if constexpr (WHAT == 1) window_dq_row<MAX_R, T>(a, b, i, h, lane);
+  if constexpr (WHAT == 2) window_dkv_row<MAX_R, T>(a, b, i, h, lane);
+  if constexpr (WHAT == 3) {
+    const T* o = strided_row((const T*)a.ctx, a.sc, b, i, h);
+    const T* d = strided_row((const T*)a.dctx, a.sc, b, i, h);
+    float s = 0.f;
+    for (int k = lane; k < a.dh; k += 64) s = fmaf(to_f(o[k]), to_f(d[k]), s);
+    s = wave_sum(s);
+    if (lane == 0) a.delta[((long long)b * a.H + h) * a.Sq + i] = s;
+  }
+}
+
+template <int WHAT>
+static int rows_launch(const WindowArgs& a, int dtype, hipStream_t s) {
+  const long long rows = (long long)a.B * (WHAT == 2 ? (long long)a.Sk * a.Hkv : (long long)a.Sq * a.H);
+  const dim3 grid((unsigned)((rows + 3) / 4));
+  if (dtype == FAX_F32) hipLaunchKernelGGL((window_rows_kernel<float, WHAT>), grid, dim3(256), 0, s, a);
+  else hipLaunchKernelGGL((window_rows_kernel<bf16_t, WHAT>), grid, dim3(256), 0, s, a);
+  return FAX_OK;
+}
+
+static WindowArgs window_args(const FaxWindowDims& d) {
+  WindowArgs a = {};
+  a.B = d.B; a.Sq = d.Sq; a.Sk = d.Sk; a.H = d.H; a.Hkv = d.Hkv; a.group = d.H / d.Hkv; a.dh = d.dh;
+  a.window = d.window < (1 << 30) ? d.window : 1 << 30;
+  a.sinks = d.sinks;
+  a.scale = (float)(1.0 / sqrt((double)d.dh));
+  a.sq = d.q; a.skv = d.kv; a.sc = d.ctx;
+  return a;
+}
+
+size_t window_ws_bytes(const FaxWindowDims& d) { return ((size_t)d.B * d.H * d.Sq * 4 + 255) / 256 * 256; }
+
+// Pairs of a whole batch without k_len and q_pos: what the timing report counts.
+static double window_pairs(const FaxWindowDims& d) {
+  double n = 0.0;
+  const long long first = (long long)d.Sk - d.Sq;
+  // query at p sees min(p + 1, window) keys and the sinks before them
+  for (int part = 0; part < 2; part++) {
+    const long long cap = part ? d.sinks : d.window, shift = part ? d.window : 0;
+    const long long a = first + 1 - shift, b = (long long)d.Sk - shift;  // terms min(max(x, 0), cap), x = a .. b
+    const long long lo = a > 1 ? a : 1, mid = b < cap ? b : cap;
+    if (mid >= lo) n += 0.5 * (double)(lo + mid) * (double)(mid - lo + 1);
+    const long long flat = (lo > cap + 1 ? lo : cap + 1);
+    if (b >= flat) n += (double)cap * (double)(b - flat + 1);
+  }
+  return n * d.B * d.H;
+}
+
+int window_fwd(const FaxWindowDims& d, const void* q, const void* k, const void* v, const int32_t* q_pos, const int32_t* k_len, void* ctx,
+               float* lse, void* ws, hipStream_t s) {
+  (void)ws;
+  Timed t_("window_attention_fwd", WORK_FLOP, 4.0 * d.dh * window_pairs(d), s);
+  WindowArgs a = window_args(d);
+  a.q = q; a.k = k; a.v = v; a.q_pos = q_pos; a.k_len = k_len; a.ctx = ctx; a.lse = lse;
+  FAX_TRY(rows_launch<0>(a, d.dtype, s));
+  FAX_LAUNCH_CHECK("window_attention_fwd");
+  return FAX_OK;
+}
+
+int window_bwd(const FaxWindowDims& d, const void* q, const void* k, const void* v, const int32_t* q_pos, const int32_t* k_len, const void* ctx,
+               const float* lse, const void* dctx, void* dq, void* dk, void* dv, void* ws, hipStream_t s) {
+  Timed t_("window_attention_bwd", WORK_FLOP, 10.0 * d.dh * window_pairs(d), s);
+  WindowArgs a = window_args(d);
+  a.q = q; a.k = k; a.v = v; a.q_pos = q_pos; a.k_len = k_len; a.ctx = const_cast<void*>(ctx); a.lse = const_cast<float*>(lse);
+  a.dctx = dctx; a.dq = dq; a.dk = dk; a.dv = dv; a.delta = (float*)ws;
+  FAX_TRY(rows_launch<3>(a, d.dtype, s));
+  FAX_TRY(rows_launch<1>(a, d.dtype, s));
+  FAX_TRY(rows_launch<2>(a, d.dtype, s));
+  FAX_LAUNCH_CHECK("window_attention_bwd");
+  return FAX_OK;
+}
+
+}  // namespace fax
