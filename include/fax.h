@@ -469,6 +469,16 @@ typedef struct FaxWindowDims {
   int32_t window, sinks;
   FaxStrides q, kv, ctx;
 } FaxWindowDims;
+/* Host-only: what the two calls make of a size whose tensors start on 16 bytes.
+ *   form         FAX_ATTENTION_*, as in FaxAttentionRoute.
+ *   fwd_waves, dq_waves, kv_waves   wavefronts of a workgroup (32 rows each; 32 keys, 16 above head width 64): 4, or 1 where workgroups are few.
+ *   fwd_splits   runs of keys that a row's forward pass is cut into, which a second kernel joins (1: none).
+ *   sink_splits  runs of queries that the sinks' dK and dV are cut into (1: none).
+ * Exposed so that a test can assert that its sizes run the form they are about. */
+typedef struct FaxWindowRoute {
+  int32_t form, fwd_waves, fwd_splits, dq_waves, kv_waves, sink_splits;
+} FaxWindowRoute;
+int fax_window_attention_route(const FaxWindowDims* dims, FaxWindowRoute* out);
 int fax_window_attention_workspace_bytes(const FaxWindowDims* dims, size_t* out);
 int fax_window_attention_fwd(const FaxWindowDims* dims, const void* q, const void* k, const void* v, const int32_t* q_pos,
                              const int32_t* k_len, void* ctx, float* lse, void* ws, size_t ws_bytes, void* stream);

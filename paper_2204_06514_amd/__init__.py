@@ -91,6 +91,10 @@ class FaxWindowDims(C.Structure):
         (n, FaxStrides) for n in ("q", "kv", "ctx")]
 
 
+class FaxWindowRoute(C.Structure):
+    _fields_ = [(n, C.c_int32) for n in ("form", "fwd_waves", "fwd_splits", "dq_waves", "kv_waves", "sink_splits")]
+
+
 class FaxAdamWTensor(C.Structure):
     _fields_ = [(n, C.c_void_p) for n in ("master", "m", "v", "grad", "lowp", "m_scale", "v_scale")] + [
         ("n", C.c_size_t), ("grad_dtype", C.c_int32), ("decay", C.c_int32)]
@@ -154,6 +158,7 @@ def _load():
         "fax_embedding_fwd": (i32, [i32] * 4 + [vp, vp, f32, vp, vp]),
         "fax_embedding_bwd_workspace_bytes": (i32, [i32] * 3 + [P(sz)]),
         "fax_embedding_bwd": (i32, [i32] * 4 + [vp, vp, f32, vp, i32, vp, sz, vp]),
+        "fax_window_attention_route": (i32, [P(FaxWindowDims), P(FaxWindowRoute)]),
         "fax_window_attention_workspace_bytes": (i32, [P(FaxWindowDims), P(sz)]),
         "fax_window_attention_fwd": (i32, [P(FaxWindowDims)] + [vp] * 8 + [sz, vp]),
         "fax_window_attention_bwd": (i32, [P(FaxWindowDims)] + [vp] * 12 + [sz, vp]),
@@ -427,6 +432,12 @@ def _laid_out(t, dims, name, strides):
     assert t.shape == shape, "a tensor of %s where dims say %s" % (tuple(t.shape), shape)
     assert all(n == 1 or x == y for n, x, y in zip(shape, t.stride(), s + (1,))), "strides %s where dims.%s says %s" % (t.stride(), name, s)
     return t.data_ptr()
+
+
+def fax_window_attention_route(dims):
+    out = FaxWindowRoute()
+    _check(_lib.fax_window_attention_route(C.byref(dims), C.byref(out)))
+    return out
 
 
 def fax_window_attention_workspace_bytes(dims):

@@ -23,11 +23,23 @@ struct WindowArgs {
   float* delta;
 };
 
+// How a size is run (kernels_window.hip), and where its parts lie in the workspace.
+struct WindowPlan {
+  int form;                                    // FAX_ATTENTION_*
+  int fwd_waves, fwd_splits, dq_waves, kv_waves, sink_tiles, sink_splits;
+  size_t delta, part_o, part_ml, parts, total;
+};
+int window_fwd_mfma(const WindowArgs& a, int waves, int splits, float* part_o, void* part_ml, hipStream_t s);
+int window_dq_mfma(const WindowArgs& a, int waves, hipStream_t s);
+int window_dkv_keys(int dh, int waves);  // keys of a workgroup
+int window_dkv_mfma(const WindowArgs& a, int waves, int sink_tiles, int splits, float* parts, hipStream_t s);
+
 struct WindowSeq {
   int pos0, k_len;
   __device__ __forceinline__ WindowSeq(const WindowArgs& a, int b) {
-    k_len = a.k_len ? min(max(a.k_len[b], 0), a.Sk) : a.Sk;
-    pos0 = a.q_pos ? min(max(a.q_pos[b], -(1 << 30)), (1 << 30) - a.Sq) : a.Sk - a.Sq;
+    // (b is the same for a wavefront: what follows from these may stay in scalar registers)
+    k_len = __builtin_amdgcn_readfirstlane(a.k_len ? min(max(a.k_len[b], 0), a.Sk) : a.Sk);
+    pos0 = __builtin_amdgcn_readfirstlane(a.q_pos ? min(max(a.q_pos[b], -(1 << 30)), (1 << 30) - a.Sq) : a.Sk - a.Sq);
   }
 };
 

@@ -1214,6 +1214,14 @@ int fax_window_attention_workspace_bytes(const FaxWindowDims* dims, size_t* out)
   return FAX_OK;
 }
 
+int fax_window_attention_route(const FaxWindowDims* dims, FaxWindowRoute* out) {
+  FaxWindowDims d;
+  FAX_TRY(check_window(dims, &d));
+  if (!out) { set_error("out is NULL"); return FAX_ERR_INVALID_ARG; }
+  window_route(d, out);
+  return FAX_OK;
+}
+
 static int check_window_ws(const FaxWindowDims& d, const void* ws, size_t ws_bytes) {
   FAX_TRY(check_ptr(ws, "ws"));
   const size_t need = window_ws_bytes(d);

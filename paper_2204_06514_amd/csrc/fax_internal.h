@@ -268,6 +268,7 @@ int embedding_bwd(int dtype, int N, int V, int D, const int32_t* tokens, const v
 
 // ---- attention in a window (dims checked, with their strides filled in) ----------------------------
 size_t window_ws_bytes(const FaxWindowDims& d);
+void window_route(const FaxWindowDims& d, FaxWindowRoute* out);
 int window_fwd(const FaxWindowDims& d, const void* q, const void* k, const void* v, const int32_t* q_pos, const int32_t* k_len, void* ctx,
                float* lse, void* ws, hipStream_t s);
 int window_bwd(const FaxWindowDims& d, const void* q, const void* k, const void* v, const int32_t* q_pos, const int32_t* k_len, const void* ctx,

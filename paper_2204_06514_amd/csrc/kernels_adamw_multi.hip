@@ -108,19 +108,22 @@ __device__ __forceinline__ void store4(uint8_t* p, size_t i, size_t n, uint32_t 
 
 __device__ __forceinline__ bool finite(float x) { return fabsf(x) <= 3.4028235e38f; }
 
-// One element.  The multiply-adds are spelled out, so that an element's bits do not depend on its place.
+// One element.  Every product and sum is rounded by itself (no contraction into multiply-adds): an element's bits do not depend on its place
+// or on the compiler, and a code of eight bits that hangs on the last of them can be computed again anywhere.
 __device__ __forceinline__ void update(float g, float& p, float& m, float& v, const AdamScalars& a) {
-  m = fmaf(a.b1, m, a.one_m_b1 * g);
-  v = fmaf(a.b2, v, a.one_m_b2 * g * g);
+#pragma clang fp contract(off)
+  m = a.b1 * m + a.one_m_b1 * g;
+  v = a.b2 * v + a.one_m_b2 * g * g;
   const float root = sqrtf(v * a.inv_bc2) + a.eps;
-  p = fmaf(p, a.decay, -(a.lr * (m * a.inv_bc1) / root));
+  const float up = m * a.inv_bc1 / root;
+  p = p * a.decay - a.lr * up;
 }
 
 // x in [0, 448] or NaN, up or down to an e4m3 number: up where the bits cut off and the random ones carry.  Those are the last twenty of
 // an fp32 number of at least 2^-6; below, e4m3 numbers are whole multiples of 2^-9, as they are from 2^-6 to 2^-5.
 __device__ __forceinline__ float round_random(float x, uint32_t bits20) {
   const bool low = x < 0.015625f;
-  float y = low ? x + 0.015625f : x;
+  float y = low ? x + 0.015625f : x;  // (2^-6)
   y = __uint_as_float((__float_as_uint(y) + bits20) & 0xfff00000u);
   y = low ? y - 0.015625f : y;
   return fminf(y, E4M3_MAX);
@@ -183,7 +186,7 @@ __global__ __launch_bounds__(256) void adamw_table_kernel(MultiTable b, AdamScal
       m_top = wave_max(m_top);
       v_top = wave_max(v_top);
       if (m_top < M_FLOOR) m_top = 0.f;
-      const float m_inv = m_top > 0.f ? E4M3_MAX / m_top : 0.f, v_inv = v_top > 0.f ? E4M3_MAX / v_top : 0.f;
+      const float m_inv = m_top > 0.f ? 1.f / m_top * E4M3_MAX : 0.f, v_inv = v_top > 0.f ? 1.f / v_top * E4M3_MAX : 0.f;
 #pragma unroll
       for (int q = 0; q < 4; q++) {
         const float nan = __builtin_nanf("");
@@ -195,8 +198,8 @@ __global__ __launch_bounds__(256) void adamw_table_kernel(MultiTable b, AdamScal
       store4((uint8_t*)e.m, i, n, pack4(m));
       store4((uint8_t*)e.v, i, n, pack4(v));
       if (lane == 0) {
-        e.m_scale[at] = m_top / E4M3_MAX;
-        e.v_scale[at] = v_top / E4M3_MAX;
+        e.m_scale[at] = m_top * (1.f / E4M3_MAX);
+        e.v_scale[at] = v_top * (1.f / E4M3_MAX);
       }
     }
     store4(e.p, i, n, p);

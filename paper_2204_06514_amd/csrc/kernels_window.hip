@@ -1,5 +1,7 @@
 // Attention in a sliding window with sinks: the scalar kernels, one wavefront to a row, for any head width up to 256 and any
 // alignment, and the choice between them and the matrix-core kernels.
+#include <initializer_list>
+
 #include "attn_window.h"
 
 namespace fax {
@@ -46,7 +48,66 @@ static WindowArgs window_args(const FaxWindowDims& d) {
   return a;
 }
 
-size_t window_ws_bytes(const FaxWindowDims& d) { return ((size_t)d.B * d.H * d.Sq * 4 + 255) / 256 * 256; }
+// Rows on 16 bytes, whole 16-byte chunks to a head, offsets within a tile of 64 rows in 32 bits.
+static bool strides_fit(const FaxStrides& s) { return s.batch % 8 == 0 && s.row % 8 == 0 && s.head % 8 == 0 && s.row <= (1 << 24); }
+
+static WindowPlan window_plan(const FaxWindowDims& d) {
+  WindowPlan p = {};
+  p.form = FAX_ATTENTION_SCALAR;
+  p.fwd_waves = p.dq_waves = p.kv_waves = 4;
+  p.fwd_splits = p.sink_splits = 1;
+  const bool fits = strides_fit(d.q) && strides_fit(d.kv) && strides_fit(d.ctx);
+  const long long heads = (long long)d.B * d.Hkv, rows = (long long)d.Sq * (d.H / d.Hkv);
+  if (d.dtype == FAX_BF16 && d.dh % 8 == 0 && d.dh <= 128 && fits && rows < (1 << 30)) {
+    p.form = d.dh == 64 || d.dh == 128 ? FAX_ATTENTION_MFMA : FAX_ATTENTION_EDGE;
+    const long long t128 = (rows + 127) / 128 * heads, t32 = (rows + 31) / 32 * heads;
+    const bool few = t128 < 256;
+    p.fwd_waves = p.dq_waves = few ? 1 : 4;
+    // tiles of keys that a row meets
+    const long long seen = (long long)d.window + d.sinks + 128 < d.Sk ? d.window + d.sinks + 128 : d.Sk;
+    const long long key_tiles = (seen + 63) / 64;
+    if (few && t32 < 512) {
+      long long splits = 512 / t32;
+      if (splits > key_tiles / 2) splits = key_tiles / 2;
+      if (splits > 64) splits = 64;
+      p.fwd_splits = splits > 1 ? (int)splits : 1;
+    }
+    p.kv_waves = (d.Sk + window_dkv_keys(d.dh, 4) - 1) / window_dkv_keys(d.dh, 4) * heads < 256 ? 1 : 4;
+    const int keys = window_dkv_keys(d.dh, p.kv_waves), n = (d.Sk + keys - 1) / keys;
+    const int sinks = d.sinks < d.Sk ? d.sinks : d.Sk;
+    p.sink_tiles = (sinks + keys - 1) / keys;
+    const long long usual = (long long)d.window + keys + 64;
+    if (2 * p.sink_tiles <= n && d.Sq > usual) p.sink_splits = (int)(d.Sq / usual + 1 < 32 ? d.Sq / usual + 1 : 32);
+    if (p.sink_tiles == 0) p.sink_splits = 1;
+    if (p.sink_splits == 1) p.sink_tiles = 0;
+  }
+  size_t o = 0;
+  auto take = [&](size_t bytes) { const size_t r = o; o += (bytes + 255) / 256 * 256; return r; };
+  // forward pass and backward pass take turns in the workspace
+  const size_t all_rows = (size_t)d.B * d.H * d.Sq;
+  if (p.fwd_splits > 1) {
+    p.part_o = take(all_rows * p.fwd_splits * d.dh * 4);
+    p.part_ml = take(all_rows * p.fwd_splits * 8);
+  }
+  const size_t fwd = o;
+  o = 0;
+  p.delta = take(all_rows * 4);
+  if (p.sink_splits > 1) p.parts = take((size_t)p.sink_splits * heads * p.sink_tiles * window_dkv_keys(d.dh, p.kv_waves) * 2 * d.dh * 4);
+  p.total = o > fwd ? o : fwd;
+  return p;
+}
+size_t window_ws_bytes(const FaxWindowDims& d) { return window_plan(d).total; }
+void window_route(const FaxWindowDims& d, FaxWindowRoute* out) {
+  const WindowPlan p = window_plan(d);
+  out->form = p.form;
+  out->fwd_waves = p.fwd_waves; out->fwd_splits = p.fwd_splits; out->dq_waves = p.dq_waves; out->kv_waves = p.kv_waves;
+  out->sink_splits = p.sink_splits;
+}
+static bool on16(std::initializer_list<const void*> p) {
+  uintptr_t all = 0;
+  for (const void* x : p) all |= (uintptr_t)x;
+  return (all & 15) == 0;
+}
 
 // Pairs of a whole batch without k_len and q_pos: what the timing report counts.
 static double window_pairs(const FaxWindowDims& d) {
@@ -66,11 +127,13 @@ static double window_pairs(const FaxWindowDims& d) {
 
 int window_fwd(const FaxWindowDims& d, const void* q, const void* k, const void* v, const int32_t* q_pos, const int32_t* k_len, void* ctx,
                float* lse, void* ws, hipStream_t s) {
-  (void)ws;
   Timed t_("window_attention_fwd", WORK_FLOP, 4.0 * d.dh * window_pairs(d), s);
   WindowArgs a = window_args(d);
   a.q = q; a.k = k; a.v = v; a.q_pos = q_pos; a.k_len = k_len; a.ctx = ctx; a.lse = lse;
-  FAX_TRY(rows_launch<0>(a, d.dtype, s));
+  const WindowPlan p = window_plan(d);
+  char* w = (char*)ws;
+  if (p.form != FAX_ATTENTION_SCALAR && on16({q, k, v, ctx})) FAX_TRY(window_fwd_mfma(a, p.fwd_waves, p.fwd_splits, (float*)(w + p.part_o), w + p.part_ml, s));
+  else FAX_TRY(rows_launch<0>(a, d.dtype, s));
   FAX_LAUNCH_CHECK("window_attention_fwd");
   return FAX_OK;
 }
@@ -80,10 +143,18 @@ int window_bwd(const FaxWindowDims& d, const void* q, const void* k, const void*
   Timed t_("window_attention_bwd", WORK_FLOP, 10.0 * d.dh * window_pairs(d), s);
   WindowArgs a = window_args(d);
   a.q = q; a.k = k; a.v = v; a.q_pos = q_pos; a.k_len = k_len; a.ctx = const_cast<void*>(ctx); a.lse = const_cast<float*>(lse);
-  a.dctx = dctx; a.dq = dq; a.dk = dk; a.dv = dv; a.delta = (float*)ws;
-  FAX_TRY(rows_launch<3>(a, d.dtype, s));
-  FAX_TRY(rows_launch<1>(a, d.dtype, s));
-  FAX_TRY(rows_launch<2>(a, d.dtype, s));
+  const WindowPlan p = window_plan(d);
+  char* w = (char*)ws;
+  a.dctx = dctx; a.dq = dq; a.dk = dk; a.dv = dv; a.delta = (float*)(w + p.delta);
+  if (p.form != FAX_ATTENTION_SCALAR && on16({q, k, v, ctx, dctx, dq, dk, dv})) {
+    // dQ first: it also leaves delta, which dK and dV need
+    FAX_TRY(window_dq_mfma(a, p.dq_waves, s));
+    FAX_TRY(window_dkv_mfma(a, p.kv_waves, p.sink_tiles, p.sink_splits, (float*)(w + p.parts), s));
+  } else {
+    FAX_TRY(rows_launch<3>(a, d.dtype, s));
+    FAX_TRY(rows_launch<1>(a, d.dtype, s));
+    FAX_TRY(rows_launch<2>(a, d.dtype, s));
+  }
   FAX_LAUNCH_CHECK("window_attention_bwd");
   return FAX_OK;
 }

@@ -1,0 +1,430 @@
+// Attention in a sliding window with sinks on the CDNA4 matrix cores, bf16: dK and dV (window_mfma.h).  Two forms, as in the full
+// causal attention: up to head width 64 a wave has 32 keys (32x32x16 products), above it 16 (16x16x32), so that two workgroups share a CU.
+#include "window_mfma.h"
+
+namespace fax {
+
+// What both forms have in common: the stream of query tiles and its loads.
+template <int DH, int WAVES, bool SWZ16, bool EDGE>
+struct QueryStream {
+  static constexpr int NSEG = DH / 8 / WAVES, TB = TR * DH * 2, LD_OFF = 2 * TB, STAGE = 2 * TB + 4 * 256;
+  const WindowArgs& a;
+  int b, hk, wave, lane;
+  int i_first, per_head, n;  // first query of a head's first tile; tiles of a head; of all heads
+  unsigned sm;
+  TileLoads<DH, WAVES, SWZ16> q, dout;
+  bool in_head[NSEG];
+  __device__ __forceinline__ QueryStream(const WindowArgs& a_, int b_, int hk_, const QueryRange& r, int wave_, unsigned sm_, int nch)
+      : a(a_), q(wave_, a_.sq.row), dout(wave_, a_.sc.row) {
+    b = b_; hk = hk_; wave = wave_; sm = sm_;
+    lane = threadIdx.x & 63;
+    i_first = r.i0 / TR * TR;
+    per_head = r.i0 < r.i1 ? (r.i1 - i_first + TR - 1) / TR : 0;
+    n = per_head * a.group;
+#pragma unroll
+    for (int i = 0; i < NSEG; i++) in_head[i] = !EDGE || lane_in_head<DH, WAVES, SWZ16>(wave, i, nch);
+  }
+  __device__ __forceinline__ int query(int u) const { return i_first + u % per_head * TR; }
+  __device__ __forceinline__ int head(int u) const { return hk * a.group + u / per_head; }
+  // Tile u into buffer `buf`: segments of Q and dO, then lse and delta (lanes 0-15 lse, 16-31 delta, the others the same again).
+  __device__ __forceinline__ void load(int u, int buf) const {
+    const int i0 = query(u), h = head(u), rows = a.Sq - i0;
+    const unsigned st = sm + buf * STAGE;
+    const bf16_t* qt = strided_row((const bf16_t*)a.q, a.sq, b, i0, h);
+    const bf16_t* dt = strided_row((const bf16_t*)a.dctx, a.sc, b, i0, h);
+#pragma unroll
+    for (int i = 0; i < NSEG; i++)
+      if (in_head[i]) {
+        q.segment(qt, rows, st, i);
+        dout.segment(dt, rows, st + TB, i);
+      }
+    const long long stat = ((long long)b * a.H + h) * a.Sq + i0;
+#pragma unroll
+    for (int i = 0; i < 4 / WAVES; i++) {
+      const int rb = wave * (4 / WAVES) + i;  // sixteen rows
+      lds_dma4(((lane & 16) ? a.delta : a.lse) + stat + min(rb * 16 + (lane & 15), rows - 1), st + LD_OFF + rb * 256);
+    }
+  }
+  // lse or delta of the four rows from `row` on
+  __device__ __forceinline__ static float4 stat4(const char* st, int row, int which) {
+    return *reinterpret_cast<const float4*>(st + LD_OFF + (row >> 4) * 256 + which * 64 + (row & 15) * 4);
+  }
+};
+
+// Where a key's sums go: dK and dV, or a part's row of scratch ([part, head, key of the sink tiles, dK | dV, feature]).
+__device__ __forceinline__ float* part_row(const WindowArgs& a, const KeyGrid& k, float* parts, int split, int bh, int keys, int j) {
+  return parts + ((((long long)split * a.B * a.Hkv + bh) * keys + j) * 2) * a.dh;
+}
+
+// ---------------------------------------------------------------------------------------------
+// 32 keys to a wave.  Per 32-query half: S = Q K^T and dP = dO V^T, P and dS, dV^T += dO^T P and dK^T += Q^T dS.
+// ---------------------------------------------------------------------------------------------
+template <int DW, bool EDGE, int WPG>
+__global__ __launch_bounds__(64 * WPG, 2) void window_dkv_mfma_kernel(WindowArgs a, KeyGrid kg, float* __restrict__ parts) {
+  constexpr int DH = row_width<DW>();
+  typedef QueryStream<DH, WPG, false, EDGE> Stream;
+  constexpr int KS = DW / 16, DT = DW / 32, TB = Stream::TB;
+  constexpr int N = 2 * KS, LEAD = N < 8 ? N : 8;
+  static_assert(N % LEAD == 0 && N > 0, "slot plan");
+  constexpr int RT = 32 * WPG;
+  extern __shared__ __attribute__((aligned(16))) char smem[];
+  const KeyItem it_(kg, a.B * a.Hkv, blockIdx.x, gridDim.x);
+  if (!it_.ok) return;
+  const int b = it_.bh / a.Hkv, hk = it_.bh % a.Hkv;
+  const WindowSeq sq(a, b);
+  const int lane = threadIdx.x & 63, g = lane >> 5;
+  const int wave = WPG == 1 ? 0 : __builtin_amdgcn_readfirstlane(threadIdx.x >> 6);
+  const int hw = EDGE ? a.dh : DW, nch = hw / 8;
+  const float scale = a.scale, c = scale * LOG2E;
+  if (EDGE) clear_lds(smem, 2 * Stream::STAGE);
+  const int j0w = it_.tile * RT + wave * 32, jk = j0w + (lane & 31);
+  Stream qs(a, b, hk, QueryRange(a, sq, it_.tile * RT, min((it_.tile + 1) * RT, a.Sk)), wave, lds_addr(smem), nch);
+  const int u0 = it_.split < 0 ? 0 : (int)((long long)qs.n * it_.split / kg.splits);
+  const int u1 = it_.split < 0 ? qs.n : (int)((long long)qs.n * (it_.split + 1) / kg.splits);
+
+  bf16x8 kf[KS], vf[KS];
+  const bool key_ok = jk < sq.k_len;
+  const bf16_t* kp = strided_row((const bf16_t*)a.k, a.skv, b, min(jk, a.Sk - 1), hk);
+  const bf16_t* vp = strided_row((const bf16_t*)a.v, a.skv, b, min(jk, a.Sk - 1), hk);
+#pragma unroll
+  for (int ks = 0; ks < KS; ks++) {
+    const bool ok = key_ok && (!EDGE || ks * 2 + g < nch);
+    kf[ks] = __builtin_bit_cast(bf16x8, edge_load16(kp + ks * 16 + g * 8, ok));
+    vf[ks] = __builtin_bit_cast(bf16x8, edge_load16(vp + ks * 16 + g * 8, ok));
+  }
+#pragma unroll
+  for (int ks = 0; ks < KS; ks++) { settle(kf[ks]); settle(vf[ks]); }
+  f32x16 dk[DT], dv[DT];
+#pragma unroll
+  for (int dt = 0; dt < DT; dt++)
+#pragma unroll
+    for (int v = 0; v < 16; v++) dk[dt][v] = dv[dt][v] = 0.f;
+  // queries that see this lane's key
+  const QueryRange mine(a, sq, jk, jk + 1);
+  const f32x16 zero = {0.f, 0.f, 0.f, 0.f, 0.f, 0.f, 0.f, 0.f, 0.f, 0.f, 0.f, 0.f, 0.f, 0.f, 0.f, 0.f};
+  auto tile = [&](auto mask_c, int i0, int buf) {
+    constexpr bool MASK = decltype(mask_c)::value;
+    int lane_t = lane;
+    settle(lane_t);  // fragment addresses are formed tile by tile: kept from tile to tile they are some thirty registers
+    const char* st = smem + buf * Stream::STAGE;
+    auto row_frag = [&](int it, int i) { return frag_rows<DH>(i % 2 ? st + TB : st, it * 32, i / 2, lane_t); };
+    auto col_frag = [&](int it, int i) { return frag_cols<DH>(i % 2 ? st : st + TB, ((i / 2) % DT) * 32, it * 32 + (i / (2 * DT)) * 16, lane_t); };
+    bf16x8 f[LEAD];
+#pragma unroll
+    for (int i = 0; i < LEAD; i++) f[i] = row_frag(0, i);
+    __builtin_amdgcn_sched_barrier(0);
+#pragma unroll
+    for (int it = 0; it < 2; it++) {
+      f32x16 sc, dp;
+      __builtin_amdgcn_s_setprio(1);
+#pragma unroll
+      for (int i = 0; i < N; i++) {
+        if (i % 2 == 0) sc = __builtin_amdgcn_mfma_f32_32x32x16_bf16(f[i % LEAD], kf[i / 2], i < 2 ? zero : sc, 0, 0, 0);
+        else dp = __builtin_amdgcn_mfma_f32_32x32x16_bf16(f[i % LEAD], vf[i / 2], i < 2 ? zero : dp, 0, 0, 0);
+        if (i + LEAD < N) f[i % LEAD] = row_frag(it, i + LEAD);
+        else f[i % LEAD] = col_frag(it, i + LEAD - N);
+        __builtin_amdgcn_sched_barrier(0);
+      }
+      bf16x8 pb[2], db[2];  // P and dS as factors: bf16, half a step off
+      __builtin_amdgcn_s_setprio(0);
+#pragma unroll
+      for (int q = 0; q < 4; q++) {
+        const float4 l4 = Stream::stat4(st, it * 32 + q * 8 + g * 4, 0), d4 = Stream::stat4(st, it * 32 + q * 8 + g * 4, 1);
+#pragma unroll
+        for (int r = 0; r < 4; r++) {
+          const int v = q * 4 + r, i = i0 + it * 32 + q * 8 + g * 4 + r;
+          float e = __builtin_amdgcn_exp2f(fmaf(sc[v], c, -LOG2E * f4_get(l4, r)));
+          float d = e * (dp[v] - f4_get(d4, r));
+          if (MASK) {
+            const bool out = (i < mine.i0) | (i >= mine.i1);
+            e = out ? 0.f : e;
+            d = out ? 0.f : d;
+          }
+          pb[v >> 3][v & 7] = (__bf16)e;
+          db[v >> 3][v & 7] = (__bf16)d;
+        }
+      }
+      __builtin_amdgcn_sched_barrier(0);
+      __builtin_amdgcn_s_setprio(1);
+#pragma unroll
+      for (int i = 0; i < N; i++) {
+        const int hh = i / (2 * DT), dt = (i / 2) % DT;
+        if (i % 2 == 0) dv[dt] = __builtin_amdgcn_mfma_f32_32x32x16_bf16(f[i % LEAD], pb[hh], dv[dt], 0, 0, 0);
+        else dk[dt] = __builtin_amdgcn_mfma_f32_32x32x16_bf16(f[i % LEAD], db[hh], dk[dt], 0, 0, 0);
+        if (i + LEAD < N) f[i % LEAD] = col_frag(it, i + LEAD);
+        else if (it == 0) f[i % LEAD] = row_frag(1, i + LEAD - N);
+        __builtin_amdgcn_sched_barrier(0);
+      }
+    }
+    __builtin_amdgcn_s_setprio(0);
+  };
+
+  if (u0 < u1) {
+    qs.load(u0, 0);
+    lds_dma_wait();
+    __syncthreads();
+    for (int u = u0; u < u1; u++) {
+      const int i0 = qs.query(u), buf = (u - u0) & 1, rows = a.Sq - i0;
+      if (u + 1 < u1) qs.load(u + 1, buf ^ 1);
+      const int p0 = sq.pos0 + i0, p1 = p0 + min(TR, rows) - 1;
+      if (rows >= TR && sees_all(a, sq.k_len, p0, p1, j0w, 32)) {
+        tile(F_{}, i0, buf);
+      } else if (sees_any(a, sq.k_len, p0, p1, j0w, 32)) {
+        tile(T_{}, i0, buf);
+      }
+      lds_dma_wait();
+      __syncthreads();
+    }
+  }
+
+  if (it_.split >= 0) {
+    float* o = part_row(a, kg, parts, it_.split, it_.bh, kg.sink_tiles * RT, jk);
+#pragma unroll
+    for (int dt = 0; dt < DT; dt++)
+#pragma unroll
+      for (int q = 0; q < 4; q++) {
+        const int d = dt * 32 + q * 8 + g * 4;
+        if (EDGE && dt * 32 + q * 8 >= hw) continue;
+        *reinterpret_cast<float4*>(o + d) = make_float4(dk[dt][q * 4], dk[dt][q * 4 + 1], dk[dt][q * 4 + 2], dk[dt][q * 4 + 3]);
+        *reinterpret_cast<float4*>(o + a.dh + d) = make_float4(dv[dt][q * 4], dv[dt][q * 4 + 1], dv[dt][q * 4 + 2], dv[dt][q * 4 + 3]);
+      }
+    return;
+  }
+  const bool store = jk < a.Sk;
+  const unsigned long long odd = __builtin_amdgcn_ballot_w64(store && not_finite(dv, not_finite(dk, 0.f)) != 0.f);
+  unsigned again = (unsigned)odd | (unsigned)(odd >> 32);
+  if (store && !((again >> (lane & 31)) & 1)) {
+    store_rows<DW, EDGE>(strided_row((bf16_t*)a.dk, a.skv, b, jk, hk), dk, scale, g, hw);
+    store_rows<DW, EDGE>(strided_row((bf16_t*)a.dv, a.skv, b, jk, hk), dv, 1.f, g, hw);
+  }
+  for (; again; again &= again - 1) {
+    int lane_r = lane;
+    settle(lane_r);
+    window_dkv_row<(DW + 63) / 64, bf16_t>(a, b, j0w + __builtin_ctz(again), hk, lane_r);
+  }
+}
+
+// ---------------------------------------------------------------------------------------------
+// 16 keys to a wave (head widths above 64).
+// ---------------------------------------------------------------------------------------------
+template <int DW, bool EDGE, int WPG>
+__global__ __launch_bounds__(64 * WPG, 2) void window_dkv16_mfma_kernel(WindowArgs a, KeyGrid kg, float* __restrict__ parts) {
+  constexpr int DH = row_width<DW>();
+  typedef QueryStream<DH, WPG, true, EDGE> Stream;
+  constexpr int KS = DW / 32, DT = DW / 16, TB = Stream::TB;
+  constexpr int N = 4 * KS, LEAD = N % 8 == 0 ? 8 : 6;
+  static_assert(N == 2 * DT && N % LEAD == 0 && N > 0, "slot plan");
+  constexpr int RT = 16 * WPG;
+  extern __shared__ __attribute__((aligned(16))) char smem[];
+  const KeyItem it_(kg, a.B * a.Hkv, blockIdx.x, gridDim.x);
+  if (!it_.ok) return;
+  const int b = it_.bh / a.Hkv, hk = it_.bh % a.Hkv;
+  const WindowSeq sq(a, b);
+  const int lane = threadIdx.x & 63, gq = lane >> 4;
+  const int wave = WPG == 1 ? 0 : __builtin_amdgcn_readfirstlane(threadIdx.x >> 6);
+  const int hw = EDGE ? a.dh : DW, nch = hw / 8;
+  const float scale = a.scale, c = scale * LOG2E;
+  if (EDGE) clear_lds(smem, 2 * Stream::STAGE);
+  const int j0w = it_.tile * RT + wave * 16, jk = j0w + (lane & 15);
+  Stream qs(a, b, hk, QueryRange(a, sq, it_.tile * RT, min((it_.tile + 1) * RT, a.Sk)), wave, lds_addr(smem), nch);
+  const int u0 = it_.split < 0 ? 0 : (int)((long long)qs.n * it_.split / kg.splits);
+  const int u1 = it_.split < 0 ? qs.n : (int)((long long)qs.n * (it_.split + 1) / kg.splits);
+
+  bf16x8 kf[KS], vf[KS];
+  const bool key_ok = jk < sq.k_len;
+  const bf16_t* kp = strided_row((const bf16_t*)a.k, a.skv, b, min(jk, a.Sk - 1), hk);
+  const bf16_t* vp = strided_row((const bf16_t*)a.v, a.skv, b, min(jk, a.Sk - 1), hk);
+#pragma unroll
+  for (int ks = 0; ks < KS; ks++) {
+    const bool ok = key_ok && (!EDGE || ks * 4 + gq < nch);
+    kf[ks] = __builtin_bit_cast(bf16x8, edge_load16(kp + ks * 32 + gq * 8, ok));
+    vf[ks] = __builtin_bit_cast(bf16x8, edge_load16(vp + ks * 32 + gq * 8, ok));
+  }
+#pragma unroll
+  for (int ks = 0; ks < KS; ks++) { settle(kf[ks]); settle(vf[ks]); }
+  f32x4 dk[DT], dv[DT];
+#pragma unroll
+  for (int dt = 0; dt < DT; dt++)
+#pragma unroll
+    for (int r = 0; r < 4; r++) dk[dt][r] = dv[dt][r] = 0.f;
+  const QueryRange mine(a, sq, jk, jk + 1);
+  const f32x4 zero = {0.f, 0.f, 0.f, 0.f};
+  auto tile = [&](auto mask_c, int i0, int buf) {
+    constexpr bool MASK = decltype(mask_c)::value;
+    int lane_t = lane;
+    settle(lane_t);  // fragment addresses are formed tile by tile: kept from tile to tile they are some thirty registers
+    const char* st = smem + buf * Stream::STAGE;
+    auto row_frag = [&](int it, int i) { return frag_rows16<DH>(i % 2 ? st + TB : st, it * 32 + ((i / 2) / KS) * 16, (i / 2) % KS, lane_t); };
+    auto col_frag = [&](int it, int i) { return frag_cols16<DH>(i % 2 ? st : st + TB, (i / 2) * 16, it * 32, lane_t); };
+    bf16x8 f[LEAD];
+#pragma unroll
+    for (int i = 0; i < LEAD; i++) f[i] = row_frag(0, i);
+    __builtin_amdgcn_sched_barrier(0);
+#pragma unroll
+    for (int it = 0; it < 2; it++) {
+      f32x4 sc[2], dp[2];
+      __builtin_amdgcn_s_setprio(1);
+#pragma unroll
+      for (int i = 0; i < N; i++) {
+        const int qg = (i / 2) / KS, ks = (i / 2) % KS;
+        if (i % 2 == 0) sc[qg] = __builtin_amdgcn_mfma_f32_16x16x32_bf16(f[i % LEAD], kf[ks], ks == 0 ? zero : sc[qg], 0, 0, 0);
+        else dp[qg] = __builtin_amdgcn_mfma_f32_16x16x32_bf16(f[i % LEAD], vf[ks], ks == 0 ? zero : dp[qg], 0, 0, 0);
+        if (i + LEAD < N) f[i % LEAD] = row_frag(it, i + LEAD);
+        else f[i % LEAD] = col_frag(it, i + LEAD - N);
+        __builtin_amdgcn_sched_barrier(0);
+      }
+      bf16x8 pb, db;
+      __builtin_amdgcn_s_setprio(0);
+#pragma unroll
+      for (int qg = 0; qg < 2; qg++) {
+        const int row = it * 32 + qg * 16 + gq * 4;
+        const float4 l4 = Stream::stat4(st, row, 0), d4 = Stream::stat4(st, row, 1);
+#pragma unroll
+        for (int r = 0; r < 4; r++) {
+          const int i = i0 + row + r;
+          float e = __builtin_amdgcn_exp2f(fmaf(sc[qg][r], c, -LOG2E * f4_get(l4, r)));
+          float d = e * (dp[qg][r] - f4_get(d4, r));
+          if (MASK) {
+            const bool out = (i < mine.i0) | (i >= mine.i1);
+            e = out ? 0.f : e;
+            d = out ? 0.f : d;
+          }
+          pb[qg * 4 + r] = (__bf16)e;
+          db[qg * 4 + r] = (__bf16)d;
+        }
+      }
+      __builtin_amdgcn_sched_barrier(0);
+      __builtin_amdgcn_s_setprio(1);
+#pragma unroll
+      for (int i = 0; i < N; i++) {
+        const int dt = i / 2;
+        if (i % 2 == 0) dv[dt] = __builtin_amdgcn_mfma_f32_16x16x32_bf16(f[i % LEAD], pb, dv[dt], 0, 0, 0);
+        else dk[dt] = __builtin_amdgcn_mfma_f32_16x16x32_bf16(f[i % LEAD], db, dk[dt], 0, 0, 0);
+        if (i + LEAD < N) f[i % LEAD] = col_frag(it, i + LEAD);
+        else if (it == 0) f[i % LEAD] = row_frag(1, i + LEAD - N);
+        __builtin_amdgcn_sched_barrier(0);
+      }
+    }
+    __builtin_amdgcn_s_setprio(0);
+  };
+
+  if (u0 < u1) {
+    qs.load(u0, 0);
+    lds_dma_wait();
+    __syncthreads();
+    for (int u = u0; u < u1; u++) {
+      const int i0 = qs.query(u), buf = (u - u0) & 1, rows = a.Sq - i0;
+      if (u + 1 < u1) qs.load(u + 1, buf ^ 1);
+      const int p0 = sq.pos0 + i0, p1 = p0 + min(TR, rows) - 1;
+      if (rows >= TR && sees_all(a, sq.k_len, p0, p1, j0w, 16)) {
+        tile(F_{}, i0, buf);
+      } else if (sees_any(a, sq.k_len, p0, p1, j0w, 16)) {
+        tile(T_{}, i0, buf);
+      }
+      lds_dma_wait();
+      __syncthreads();
+    }
+  }
+
+  if (it_.split >= 0) {
+    float* o = part_row(a, kg, parts, it_.split, it_.bh, kg.sink_tiles * RT, jk);
+#pragma unroll
+    for (int dt = 0; dt < DT; dt++) {
+      const int d = dt * 16 + gq * 4;
+      if (EDGE && d >= hw) continue;
+      *reinterpret_cast<float4*>(o + d) = make_float4(dk[dt][0], dk[dt][1], dk[dt][2], dk[dt][3]);
+      *reinterpret_cast<float4*>(o + a.dh + d) = make_float4(dv[dt][0], dv[dt][1], dv[dt][2], dv[dt][3]);
+    }
+    return;
+  }
+  const bool store = jk < a.Sk;
+  const unsigned long long odd = __builtin_amdgcn_ballot_w64(store && not_finite(dv, not_finite(dk, 0.f)) != 0.f);
+  unsigned again = (unsigned)(odd | (odd >> 16) | (odd >> 32) | (odd >> 48)) & 0xffffu;
+  if (store && !((again >> (lane & 15)) & 1)) {
+    bf16_t* ko = strided_row((bf16_t*)a.dk, a.skv, b, jk, hk);
+    bf16_t* vo = strided_row((bf16_t*)a.dv, a.skv, b, jk, hk);
+#pragma unroll
+    for (int dt = 0; dt < DT; dt++) {
+      if (EDGE && dt * 16 + gq * 4 >= hw) continue;
+      bf16x4 x, y;
+#pragma unroll
+      for (int r = 0; r < 4; r++) {
+        x[r] = (__bf16)(dk[dt][r] * scale);
+        y[r] = (__bf16)dv[dt][r];
+      }
+      *reinterpret_cast<bf16x4*>(ko + dt * 16 + gq * 4) = x;
+      *reinterpret_cast<bf16x4*>(vo + dt * 16 + gq * 4) = y;
+    }
+  }
+  for (; again; again &= again - 1) {
+    int lane_r = lane;
+    settle(lane_r);
+    window_dkv_row<2, bf16_t>(a, b, j0w + __builtin_ctz(again), hk, lane_r);
+  }
+}
+
+// The parts of the sink tiles' keys, added in order: one wavefront to a key.
+__global__ __launch_bounds__(256) void window_fold_kernel(WindowArgs a, KeyGrid kg, int tile_keys, const float* __restrict__ parts) {
+  const int keys = kg.sink_tiles * tile_keys, n = min(keys, a.Sk);
+  const int item = blockIdx.x * 4 + (threadIdx.x >> 6), lane = threadIdx.x & 63;
+  if (item >= n * a.B * a.Hkv) return;
+  const int j = item % n, bh = item / n;
+  float s[4] = {0.f, 0.f, 0.f, 0.f};  // dK and dV, two 64-wide pieces each
+  for (int p = 0; p < kg.splits; p++) {
+    const float* o = part_row(a, kg, const_cast<float*>(parts), p, bh, keys, j);
+#pragma unroll
+    for (int k = 0; k < 4; k++) {
+      const int d = lane + 64 * (k & 1);
+      if (d < a.dh) s[k] += o[(k >> 1) * a.dh + d];
+    }
+  }
+  const int b = bh / a.Hkv, hk = bh % a.Hkv;
+  if (__any((s[0] * 0.f + s[1] * 0.f) + (s[2] * 0.f + s[3] * 0.f) != 0.f)) {
+    window_dkv_row<2, bf16_t>(a, b, j, hk, lane);
+    return;
+  }
+  bf16_t* ko = strided_row((bf16_t*)a.dk, a.skv, b, j, hk);
+  bf16_t* vo = strided_row((bf16_t*)a.dv, a.skv, b, j, hk);
+#pragma unroll
+  for (int k = 0; k < 2; k++) {
+    const int d = lane + 64 * k;
+    if (d < a.dh) {
+      ko[d] = (bf16_t)(s[k] * a.scale);
+      vo[d] = (bf16_t)s[2 + k];
+    }
+  }
+}
+
+int window_dkv_keys(int dh, int waves) { return (dh <= 64 ? 32 : 16) * waves; }
+
+int window_dkv_mfma(const WindowArgs& a, int waves, int sink_tiles, int splits, float* parts, hipStream_t s) {
+  const int keys = window_dkv_keys(a.dh, waves), heads = a.B * a.Hkv;
+  KeyGrid kg;
+  kg.n_tiles = (a.Sk + keys - 1) / keys;
+  kg.sink_tiles = splits > 1 ? sink_tiles : 0;
+  kg.splits = splits;
+  kg.sink_blocks = (int)xcd_grid((long long)kg.sink_tiles * heads * splits);
+  const unsigned grid = kg.sink_blocks + xcd_grid((long long)(kg.n_tiles - kg.sink_tiles) * heads);
+  auto launch = [&](auto kern, size_t row) -> int {
+    const size_t lds = 2 * (2 * (size_t)TR * row * 2 + 4 * 256);
+    FAX_HIP(hipFuncSetAttribute(reinterpret_cast<const void*>(kern), hipFuncAttributeMaxDynamicSharedMemorySize, (int)lds));
+    hipLaunchKernelGGL(kern, dim3(grid), dim3(64 * waves), lds, s, a, kg, parts);
+    return FAX_OK;
+  };
+  auto go = [&](auto wpg) -> int {
+    constexpr int W = decltype(wpg)::value;
+    if (a.dh == 64) return launch(window_dkv_mfma_kernel<64, false, W>, 64);
+    if (a.dh == 128) return launch(window_dkv16_mfma_kernel<128, false, W>, 128);
+    if (a.dh < 64) return launch(window_dkv_mfma_kernel<64, true, W>, 64);
+    if (a.dh <= 96) return launch(window_dkv16_mfma_kernel<96, true, W>, 128);
+    return launch(window_dkv16_mfma_kernel<128, true, W>, 128);
+  };
+  FAX_TRY(waves == 1 ? go(I<1>{}) : go(I<4>{}));
+  if (kg.sink_tiles) {
+    const int n = kg.sink_tiles * keys < a.Sk ? kg.sink_tiles * keys : a.Sk;
+    hipLaunchKernelGGL(window_fold_kernel, dim3((unsigned)(((long long)n * heads + 3) / 4)), dim3(256), 0, s, a, kg, keys, parts);
+  }
+  return FAX_OK;
+}
+
+}  // namespace fax

@@ -1,0 +1,425 @@
+// Attention in a sliding window with sinks on the CDNA4 matrix cores, bf16: forward pass and dQ (window_mfma.h).
+#include "window_mfma.h"
+
+namespace fax {
+
+// ---------------------------------------------------------------------------------------------
+// Forward.  Wave w owns rows 32 w .. + 31 of the workgroup's (B operand, in registers); 64-key tiles of K and V stream through two
+// LDS buffers: S^T for both 32-key halves, online softmax over the 64 keys, O^T += V^T P^T.
+// PART: the workgroup has one of `splits` runs of the tiles and leaves its sums, undivided, with their reference point (in units of the
+// unscaled score) and their denominators, for window_join_kernel.
+// ---------------------------------------------------------------------------------------------
+template <int DW, bool EDGE, int WPG, bool PART>
+__global__ __launch_bounds__(64 * WPG, 2) void window_fwd_mfma_kernel(WindowArgs a, int n_tiles, int items, int splits, float* __restrict__ part_o,
+                                                                      float2* __restrict__ part_ml) {
+  constexpr int DH = row_width<DW>();  // row length in LDS
+  constexpr int KS = DW / 16, DT = DW / 32, TB = TR * DH * 2;
+  constexpr int N = 2 * KS;            // MFMAs per phase
+  constexpr int LEAD = N < 8 ? N : 8;  // fragments in flight
+  constexpr int NSEG = DH / 8 / WPG;   // 1 KB load instructions per wave per tile
+  extern __shared__ __attribute__((aligned(16))) char smem[];  // 2 x [K tile | V tile]
+  int item = xcd_item(blockIdx.x, gridDim.x);
+  if (item >= items) return;
+  int split = 0;
+  if (PART) { split = item % splits; item /= splits; }
+  const int tile_no = item % n_tiles, bh = item / n_tiles;
+  const int b = bh / a.Hkv, hk = bh % a.Hkv;
+  const WindowSeq sq(a, b);
+  const RowTile<WPG> rt(a, sq, b, hk, tile_no);
+  const int wave = rt.wave, lane = threadIdx.x & 63, g = lane >> 5;
+  const int hw = EDGE ? a.dh : DW, nch = hw / 8;
+  const bf16_t* kb = strided_row((const bf16_t*)a.k, a.skv, b, 0, hk);
+  const bf16_t* vb = strided_row((const bf16_t*)a.v, a.skv, b, 0, hk);
+  const float scale = a.scale, c = scale * LOG2E;
+  const unsigned sm = lds_addr(smem);
+  if (EDGE) clear_lds(smem, 4 * TB);
+
+  const KeyTiles kt(KeyRanges(a, sq, rt.p0, rt.p1));
+  const int u0 = PART ? (int)((long long)kt.n * split / splits) : 0, u1 = PART ? (int)((long long)kt.n * (split + 1) / splits) : kt.n;
+
+  bf16x8 qf[KS];
+  const bf16_t* qp = strided_row((const bf16_t*)a.q, a.sq, b, rt.i, rt.h);
+#pragma unroll
+  for (int ks = 0; ks < KS; ks++) qf[ks] = __builtin_bit_cast(bf16x8, edge_load16(qp + ks * 16 + g * 8, rt.ok && (!EDGE || ks * 2 + g < nch)));
+#pragma unroll
+  for (int ks = 0; ks < KS; ks++) settle(qf[ks]);
+  float m = -3.4028235e38f, l = 0.f;  // (a row may not see a key for a while, or at all)
+  f32x16 oacc[DT];
+#pragma unroll
+  for (int dt = 0; dt < DT; dt++)
+#pragma unroll
+    for (int v = 0; v < 16; v++) oacc[dt][v] = 0.f;
+
+  const TileLoads<DH, WPG, false> loads(wave, a.skv.row);
+  bool in_head[NSEG];
+#pragma unroll
+  for (int i = 0; i < NSEG; i++) in_head[i] = !EDGE || lane_in_head<DH, WPG, false>(wave, i, nch);
+  auto load = [&](int j0, int buf) {
+    const long long at = (long long)j0 * a.skv.row;
+#pragma unroll
+    for (int i = 0; i < NSEG; i++)
+      if (in_head[i]) {
+        loads.segment(kb + at, sq.k_len - j0, sm + buf * 2 * TB, i);
+        loads.segment(vb + at, sq.k_len - j0, sm + buf * 2 * TB + TB, i);
+      }
+  };
+  const int p = rt.p, last = min(p, sq.k_len - 1), first = p - a.window;  // sees keys in (first, last] and the sinks up to last
+  auto tile = [&](auto mask_c, int j0, int buf) {
+    constexpr bool MASK = decltype(mask_c)::value;
+    int lane_t = lane;
+    settle(lane_t);  // fragment addresses are formed tile by tile: kept from tile to tile they are some thirty registers
+    const char* kt_ = smem + buf * 2 * TB;
+    const char* vt_ = kt_ + TB;
+    auto row_frag = [&](int i) { return frag_rows<DH>(kt_, (i % 2) * 32, i / 2, lane_t); };
+    auto col_frag = [&](int i) { return frag_cols<DH>(vt_, (i % DT) * 32, ((i / DT) % 2) * 32 + ((i / DT) / 2) * 16, lane_t); };
+    bf16x8 fr[LEAD], fc[LEAD];
+#pragma unroll
+    for (int i = 0; i < LEAD; i++) fr[i] = row_frag(i);
+    f32x16 s[2];
+#pragma unroll
+    for (int jt = 0; jt < 2; jt++)
+#pragma unroll
+      for (int v = 0; v < 16; v++) s[jt][v] = 0.f;
+    __builtin_amdgcn_sched_barrier(0);
+    __builtin_amdgcn_s_setprio(1);
+#pragma unroll
+    for (int i = 0; i < N; i++) {
+      s[i % 2] = __builtin_amdgcn_mfma_f32_32x32x16_bf16(fr[i % LEAD], qf[i / 2], s[i % 2], 0, 0, 0);
+      if (i + LEAD < N) fr[i % LEAD] = row_frag(i + LEAD);
+      else fc[i + LEAD - N] = col_frag(i + LEAD - N);
+      __builtin_amdgcn_sched_barrier(0);
+    }
+    __builtin_amdgcn_s_setprio(0);
+    if (MASK) {
+#pragma unroll
+      for (int jt = 0; jt < 2; jt++)
+#pragma unroll
+        for (int v = 0; v < 16; v++) {
+          const int key = j0 + jt * 32 + (v >> 2) * 8 + g * 4 + (v & 3);
+          s[jt][v] = (key > last) | ((key <= first) & (key >= a.sinks)) ? -INFINITY : s[jt][v];
+        }
+    }
+    float mx = -INFINITY;
+#pragma unroll
+    for (int jt = 0; jt < 2; jt++)
+#pragma unroll
+      for (int v = 0; v < 16; v++) mx = fmaxf(mx, s[jt][v]);
+    mx = max32(mx);
+    // the reference point follows the running maximum lazily (at most 2^MAX_LAG above it)
+    const float mn = fmaxf(m, mx);
+    if (__builtin_amdgcn_ballot_w64((mn - m) * c > MAX_LAG) != 0) {
+      const float corr = __builtin_amdgcn_exp2f((m - mn) * c);
+      l *= corr;
+#pragma unroll
+      for (int dt = 0; dt < DT; dt++)
+#pragma unroll
+        for (int v = 0; v < 16; v++) oacc[dt][v] *= corr;
+      m = mn;
+    }
+    const float mc = m * c;
+    float rs = 0.f;
+    bf16x8 pb[2][2];  // probabilities as the second product's factors: bf16, half a step (2^-8) off each; the denominator adds them unrounded
+#pragma unroll
+    for (int jt = 0; jt < 2; jt++)
+#pragma unroll
+      for (int v = 0; v < 16; v++) {
+        const float e = __builtin_amdgcn_exp2f(fmaf(s[jt][v], c, -mc));
+        rs += e;
+        pb[jt][v >> 3][v & 7] = (__bf16)e;
+      }
+    l += sum32(rs);
+    __builtin_amdgcn_sched_barrier(0);
+    __builtin_amdgcn_s_setprio(1);
+#pragma unroll
+    for (int i = 0; i < N; i++) {
+      const int dt = i % DT, ch = i / DT;
+      oacc[dt] = __builtin_amdgcn_mfma_f32_32x32x16_bf16(fc[i % LEAD], pb[ch % 2][ch / 2], oacc[dt], 0, 0, 0);
+      if (i + LEAD < N) fc[i % LEAD] = col_frag(i + LEAD);
+      __builtin_amdgcn_sched_barrier(0);
+    }
+    __builtin_amdgcn_s_setprio(0);
+  };
+
+  if (u0 < u1) {
+    load(kt.key(u0), 0);
+    lds_dma_wait();
+    __syncthreads();
+    for (int u = u0; u < u1; u++) {
+      const int j0 = kt.key(u), buf = (u - u0) & 1;
+      if (u + 1 < u1) load(kt.key(u + 1), buf ^ 1);
+      if (sees_all(a, sq.k_len, rt.wp0, rt.wp1, j0, TR)) {
+        tile(F_{}, j0, buf);
+      } else if (sees_any(a, sq.k_len, rt.wp0, rt.wp1, j0, TR)) {
+        tile(T_{}, j0, buf);
+      }
+      lds_dma_wait();
+      __syncthreads();
+    }
+  }
+
+  const long long row_all = (long long)bh * rt.rows + rt.row;
+  if (PART) {
+    if (!rt.ok) return;
+    const long long at = row_all * splits + split;
+    if (g == 0) part_ml[at] = make_float2(m, l);
+    float* o = part_o + at * a.dh;
+#pragma unroll
+    for (int dt = 0; dt < DT; dt++)
+#pragma unroll
+      for (int q = 0; q < 4; q++) {
+        const int d = dt * 32 + q * 8 + g * 4;
+        if (!EDGE || dt * 32 + q * 8 < hw) *reinterpret_cast<float4*>(o + d) = make_float4(oacc[dt][q * 4], oacc[dt][q * 4 + 1], oacc[dt][q * 4 + 2], oacc[dt][q * 4 + 3]);
+      }
+    return;
+  }
+  const unsigned long long odd = __builtin_amdgcn_ballot_w64(rt.ok && not_finite(oacc, l * 0.f) != 0.f);
+  unsigned again = (unsigned)odd | (unsigned)(odd >> 32);
+  if (rt.ok && !((again >> (lane & 31)) & 1)) {
+    const bool none = l == 0.f;
+    store_rows<DW, EDGE>(strided_row((bf16_t*)a.ctx, a.sc, b, rt.i, rt.h), oacc, none ? 0.f : 1.f / l, g, hw);
+    if (g == 0 && a.lse) a.lse[((long long)b * a.H + rt.h) * a.Sq + rt.i] = none ? -INFINITY : m * scale + logf(l);
+  }
+  for (; again; again &= again - 1) {
+    const int src = __builtin_ctz(again);
+    int lane_r = lane;
+    settle(lane_r);
+    window_fwd_row<(DW + 63) / 64, bf16_t>(a, b, __shfl(rt.i, src, 64), __shfl(rt.h, src, 64), lane_r);
+  }
+}
+
+// ---------------------------------------------------------------------------------------------
+// dQ, and delta = dctx . ctx by row.  The same tiles; per 32-key half S^T = K Q^T and dP^T = V dO^T, dS^T = P^T (dP^T - delta), dQ^T += K^T dS^T.
+// ---------------------------------------------------------------------------------------------
+template <int DW, bool EDGE, int WPG>
+__global__ __launch_bounds__(64 * WPG, 2) void window_dq_mfma_kernel(WindowArgs a, int n_tiles, int items) {
+  constexpr int DH = row_width<DW>();
+  constexpr int KS = DW / 16, DT = DW / 32, TB = TR * DH * 2;
+  constexpr int N1 = 2 * KS, N3 = 2 * DT, LEAD = N3;
+  constexpr int NSEG = DH / 8 / WPG;
+  static_assert(N1 % LEAD == 0, "slot plan");
+  extern __shared__ __attribute__((aligned(16))) char smem[];
+  const int item = xcd_item(blockIdx.x, gridDim.x);
+  if (item >= items) return;
+  const int tile_no = item % n_tiles, bh = item / n_tiles;
+  const int b = bh / a.Hkv, hk = bh % a.Hkv;
+  const WindowSeq sq(a, b);
+  const RowTile<WPG> rt(a, sq, b, hk, tile_no);
+  const int wave = rt.wave, lane = threadIdx.x & 63, g = lane >> 5;
+  const int hw = EDGE ? a.dh : DW, nch = hw / 8;
+  const bf16_t* kb = strided_row((const bf16_t*)a.k, a.skv, b, 0, hk);
+  const bf16_t* vb = strided_row((const bf16_t*)a.v, a.skv, b, 0, hk);
+  const float scale = a.scale, c = scale * LOG2E;
+  const unsigned sm = lds_addr(smem);
+  if (EDGE) clear_lds(smem, 4 * TB);
+  const KeyTiles kt(KeyRanges(a, sq, rt.p0, rt.p1));
+
+  bf16x8 qf[KS], dof[KS];
+  const bf16_t* qp = strided_row((const bf16_t*)a.q, a.sq, b, rt.i, rt.h);
+  const bf16_t* dop = strided_row((const bf16_t*)a.dctx, a.sc, b, rt.i, rt.h);
+  const bf16_t* op = strided_row((const bf16_t*)a.ctx, a.sc, b, rt.i, rt.h);
+  const long long stat = ((long long)b * a.H + rt.h) * a.Sq + rt.i;
+  float li = rt.ok ? a.lse[stat] * LOG2E : 0.f, di = 0.f;
+#pragma unroll
+  for (int ks = 0; ks < KS; ks++) {
+    const bool ok = rt.ok && (!EDGE || ks * 2 + g < nch);
+    qf[ks] = __builtin_bit_cast(bf16x8, edge_load16(qp + ks * 16 + g * 8, ok));
+    dof[ks] = __builtin_bit_cast(bf16x8, edge_load16(dop + ks * 16 + g * 8, ok));
+    const bf16x8 o = __builtin_bit_cast(bf16x8, edge_load16(op + ks * 16 + g * 8, ok));
+#pragma unroll
+    for (int e = 0; e < 8; e++) di = fmaf((float)o[e], (float)dof[ks][e], di);
+  }
+  di = sum32(di);
+  if (g == 0 && rt.ok) a.delta[stat] = di;
+#pragma unroll
+  for (int ks = 0; ks < KS; ks++) { settle(qf[ks]); settle(dof[ks]); }
+  settle(li); settle(di);
+  f32x16 dq[DT];
+#pragma unroll
+  for (int dt = 0; dt < DT; dt++)
+#pragma unroll
+    for (int v = 0; v < 16; v++) dq[dt][v] = 0.f;
+
+  const TileLoads<DH, WPG, false> loads(wave, a.skv.row);
+  bool in_head[NSEG];
+#pragma unroll
+  for (int i = 0; i < NSEG; i++) in_head[i] = !EDGE || lane_in_head<DH, WPG, false>(wave, i, nch);
+  auto load = [&](int j0, int buf) {
+    const long long at = (long long)j0 * a.skv.row;
+#pragma unroll
+    for (int i = 0; i < NSEG; i++)
+      if (in_head[i]) {
+        loads.segment(kb + at, sq.k_len - j0, sm + buf * 2 * TB, i);
+        loads.segment(vb + at, sq.k_len - j0, sm + buf * 2 * TB + TB, i);
+      }
+  };
+  const f32x16 zero = {0.f, 0.f, 0.f, 0.f, 0.f, 0.f, 0.f, 0.f, 0.f, 0.f, 0.f, 0.f, 0.f, 0.f, 0.f, 0.f};
+  const int p = rt.p, last = min(p, sq.k_len - 1), first = p - a.window;
+  auto tile = [&](auto mask_c, int j0, int buf) {
+    constexpr bool MASK = decltype(mask_c)::value;
+    int lane_t = lane;
+    settle(lane_t);  // fragment addresses are formed tile by tile: kept from tile to tile they are some thirty registers
+    const char* kt_ = smem + buf * 2 * TB;
+    const char* vt_ = kt_ + TB;
+    auto row_frag = [&](int jt, int i) { return frag_rows<DH>((i & 1) ? vt_ : kt_, jt * 32, i / 2, lane_t); };
+    auto col_frag = [&](int jt, int i) { return frag_cols<DH>(kt_, (i % DT) * 32, jt * 32 + (i / DT) * 16, lane_t); };
+    bf16x8 f[LEAD];
+#pragma unroll
+    for (int i = 0; i < LEAD; i++) f[i] = row_frag(0, i);
+    __builtin_amdgcn_sched_barrier(0);
+#pragma unroll
+    for (int jt = 0; jt < 2; jt++) {
+      f32x16 sc, dp;
+      __builtin_amdgcn_s_setprio(1);
+#pragma unroll
+      for (int i = 0; i < N1; i++) {
+        const int ks = i / 2;
+        if (i & 1) dp = __builtin_amdgcn_mfma_f32_32x32x16_bf16(f[i % LEAD], dof[ks], i < 2 ? zero : dp, 0, 0, 0);
+        else sc = __builtin_amdgcn_mfma_f32_32x32x16_bf16(f[i % LEAD], qf[ks], i < 2 ? zero : sc, 0, 0, 0);
+        if (i + LEAD < N1) f[i % LEAD] = row_frag(jt, i + LEAD);
+        else f[i % LEAD] = col_frag(jt, i + LEAD - N1);
+        __builtin_amdgcn_sched_barrier(0);
+      }
+      bf16x8 db[2];  // dS as the second product's factor: bf16, half a step off
+      __builtin_amdgcn_s_setprio(0);
+#pragma unroll
+      for (int v = 0; v < 16; v++) {
+        const float e = __builtin_amdgcn_exp2f(fmaf(sc[v], c, -li));
+        float d = e * (dp[v] - di);
+        const int key = j0 + jt * 32 + (v >> 2) * 8 + g * 4 + (v & 3);
+        if (MASK) d = (key > last) | ((key <= first) & (key >= a.sinks)) ? 0.f : d;
+        db[v >> 3][v & 7] = (__bf16)d;
+      }
+      __builtin_amdgcn_sched_barrier(0);
+      __builtin_amdgcn_s_setprio(1);
+#pragma unroll
+      for (int i = 0; i < N3; i++) {
+        dq[i % DT] = __builtin_amdgcn_mfma_f32_32x32x16_bf16(f[i % LEAD], db[i / DT], dq[i % DT], 0, 0, 0);
+        if (jt == 0) f[i % LEAD] = row_frag(1, i);
+        __builtin_amdgcn_sched_barrier(0);
+      }
+    }
+    __builtin_amdgcn_s_setprio(0);
+  };
+
+  if (kt.n > 0) {
+    load(kt.key(0), 0);
+    lds_dma_wait();
+    __syncthreads();
+    for (int u = 0; u < kt.n; u++) {
+      const int j0 = kt.key(u), buf = u & 1;
+      if (u + 1 < kt.n) load(kt.key(u + 1), buf ^ 1);
+      if (sees_all(a, sq.k_len, rt.wp0, rt.wp1, j0, TR)) {
+        tile(F_{}, j0, buf);
+      } else if (sees_any(a, sq.k_len, rt.wp0, rt.wp1, j0, TR)) {
+        tile(T_{}, j0, buf);
+      }
+      lds_dma_wait();
+      __syncthreads();
+    }
+  }
+  const unsigned long long odd = __builtin_amdgcn_ballot_w64(rt.ok && not_finite(dq, 0.f) != 0.f);
+  unsigned again = (unsigned)odd | (unsigned)(odd >> 32);
+  if (rt.ok && !((again >> (lane & 31)) & 1)) store_rows<DW, EDGE>(strided_row((bf16_t*)a.dq, a.sq, b, rt.i, rt.h), dq, scale, g, hw);
+  if (again) __threadfence();  // delta of this wave's rows, which window_dq_row reads
+  for (; again; again &= again - 1) {
+    const int src = __builtin_ctz(again);
+    int lane_r = lane;
+    settle(lane_r);
+    window_dq_row<(DW + 63) / 64, bf16_t>(a, b, __shfl(rt.i, src, 64), __shfl(rt.h, src, 64), lane_r);
+  }
+}
+
+// Joins the parts of a row that PART workgroups left: one wavefront to a row.
+__global__ __launch_bounds__(256) void window_join_kernel(WindowArgs a, int splits, const float* __restrict__ part_o, const float2* __restrict__ part_ml,
+                                                          float octaves, float unit) {
+  const long long row = (long long)blockIdx.x * 4 + (threadIdx.x >> 6), rows = (long long)a.B * a.Hkv * a.Sq * a.group;
+  if (row >= rows) return;
+  const int lane = threadIdx.x & 63;
+  const long long per_head = (long long)a.Sq * a.group;
+  const int bh = (int)(row / per_head), r = (int)(row % per_head);
+  const int b = bh / a.Hkv, i = r / a.group, h = bh % a.Hkv * a.group + r % a.group;
+  const float2* ml = part_ml + row * splits;
+  const float* o = part_o + row * splits * a.dh;
+  float M = -3.4028235e38f;
+  for (int s = 0; s < splits; s++) M = fmaxf(M, ml[s].x);
+  float L = 0.f, acc[2] = {0.f, 0.f};
+  for (int s = 0; s < splits; s++) {
+    const float w = __builtin_amdgcn_exp2f((ml[s].x - M) * octaves);
+    L = fmaf(ml[s].y, w, L);
+#pragma unroll
+    for (int k = 0; k < 2; k++) {
+      const int d = lane + 64 * k;
+      if (d < a.dh) acc[k] = fmaf(o[(long long)s * a.dh + d], w, acc[k]);
+    }
+  }
+  if (__any(!(fabsf(acc[0]) <= 3.4028235e38f) || !(fabsf(acc[1]) <= 3.4028235e38f)) || !(L <= 3.4028235e38f)) {
+    window_fwd_row<2, bf16_t>(a, b, i, h, lane);
+    return;
+  }
+  const bool none = L == 0.f;
+  const float inv = none ? 0.f : 1.f / L;
+  bf16_t* out = strided_row((bf16_t*)a.ctx, a.sc, b, i, h);
+#pragma unroll
+  for (int k = 0; k < 2; k++) {
+    const int d = lane + 64 * k;
+    if (d < a.dh) out[d] = (bf16_t)(acc[k] * inv);
+  }
+  if (lane == 0 && a.lse) a.lse[((long long)b * a.H + h) * a.Sq + i] = none ? -INFINITY : M * unit + logf(L);
+}
+
+template <typename K>
+static int set_lds(K kern, size_t bytes) {
+  FAX_HIP(hipFuncSetAttribute(reinterpret_cast<const void*>(kern), hipFuncAttributeMaxDynamicSharedMemorySize, (int)bytes));
+  return FAX_OK;
+}
+
+// f(head width as computed, masked edges)
+template <typename F>
+static int by_width(int dh, F f) {
+  if (dh == 64) return f(I<64>{}, F_{});
+  if (dh == 128) return f(I<128>{}, F_{});
+  return dh < 64 ? f(I<64>{}, T_{}) : dh <= 96 ? f(I<96>{}, T_{}) : f(I<128>{}, T_{});
+}
+
+int window_fwd_mfma(const WindowArgs& a, int waves, int splits, float* part_o, void* part_ml, hipStream_t s) {
+  const int n_tiles = (int)(((long long)a.Sq * a.group + 32 * waves - 1) / (32 * waves));
+  const long long items = (long long)n_tiles * a.B * a.Hkv * splits;
+  return by_width(a.dh, [&](auto dw, auto edge) -> int {
+    constexpr int DW = decltype(dw)::value;
+    constexpr bool E = decltype(edge)::value;
+    constexpr size_t lds = 4 * (size_t)TR * row_width<DW>() * 2;
+    auto go = [&](auto wpg, auto part) -> int {
+      auto kern = window_fwd_mfma_kernel<DW, E, decltype(wpg)::value, decltype(part)::value>;
+      FAX_TRY(set_lds(kern, lds));
+      hipLaunchKernelGGL(kern, dim3(xcd_grid(items)), dim3(64 * waves), lds, s, a, n_tiles, (int)items, splits, part_o, (float2*)part_ml);
+      return FAX_OK;
+    };
+    if (splits > 1) {
+      FAX_TRY(waves == 1 ? go(I<1>{}, T_{}) : go(I<4>{}, T_{}));
+      const long long rows = (long long)a.B * a.H * a.Sq;
+      hipLaunchKernelGGL(window_join_kernel, dim3((unsigned)((rows + 3) / 4)), dim3(256), 0, s, a, splits, part_o, (const float2*)part_ml,
+                         a.scale * LOG2E, a.scale);
+      return FAX_OK;
+    }
+    return waves == 1 ? go(I<1>{}, F_{}) : go(I<4>{}, F_{});
+  });
+}
+
+int window_dq_mfma(const WindowArgs& a, int waves, hipStream_t s) {
+  const int n_tiles = (int)(((long long)a.Sq * a.group + 32 * waves - 1) / (32 * waves));
+  const long long items = (long long)n_tiles * a.B * a.Hkv;
+  return by_width(a.dh, [&](auto dw, auto edge) -> int {
+    constexpr int DW = decltype(dw)::value;
+    constexpr bool E = decltype(edge)::value;
+    constexpr size_t lds = 4 * (size_t)TR * row_width<DW>() * 2;
+    auto go = [&](auto wpg) -> int {
+      auto kern = window_dq_mfma_kernel<DW, E, decltype(wpg)::value>;
+      FAX_TRY(set_lds(kern, lds));
+      hipLaunchKernelGGL(kern, dim3(xcd_grid(items)), dim3(64 * waves), lds, s, a, n_tiles, (int)items);
+      return FAX_OK;
+    };
+    return waves == 1 ? go(I<1>{}) : go(I<4>{});
+  });
+}
+
+}  // namespace fax

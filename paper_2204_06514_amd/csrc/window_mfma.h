@@ -1,0 +1,132 @@
+// Attention in a window on the matrix cores (bf16): the pieces that its kernels share.  Products, registers and LDS tiles are laid out as
+// in the full causal attention (attn_mfma_common.h, attn_dkv16.h); what differs:
+//   * A workgroup of the forward pass and of dQ has 32 WPG rows of a key head: row r is query r / group, query head r % group of it.  All
+//     query heads of a key head share its K and V tiles, single tokens of grouped heads fill one wave's rows, and the rows of a workgroup span
+//     few positions, so that few tiles reach past a window's ends.
+//   * It streams the tiles of 64 keys that hold the sinks, then those that the window of some row reaches (KeyRanges).  A wave leaves out
+//     those that none of its rows sees; only those that some row sees in part take the masks.
+//   * Rows of a tile from the last key on are loads of the last key (never a read out of bounds, nothing left in LDS that was not loaded).
+#pragma once
+#include "attn_dkv16.h"
+#include "attn_window.h"
+
+namespace fax {
+
+// Workgroup -> item, with neighbouring items on one XCD (workgroups go to the eight XCDs in turn): they share K and V tiles, or Q and dO, in
+// its L2.  The grid is xcd_grid(items); items that are none are out of range.
+inline unsigned xcd_grid(long long items) { return (unsigned)((items + 7) / 8 * 8); }
+__device__ __forceinline__ int xcd_item(int block, int grid) { return (block & 7) * (grid >> 3) + (block >> 3); }
+
+// 64-key tiles of a run of queries, in order: those of the sinks, then those of the window.
+struct KeyTiles {
+  int sink_tiles, skip, n;
+  __device__ __forceinline__ KeyTiles(const KeyRanges& k) {
+    sink_tiles = (k.sink_end + TR - 1) / TR;
+    const int first = max(sink_tiles, k.lo / TR);
+    skip = first - sink_tiles;
+    n = sink_tiles + (k.lo < k.end ? max(0, (k.end + TR - 1) / TR - first) : 0);
+  }
+  __device__ __forceinline__ int key(int u) const { return (u < sink_tiles ? u : u + skip) * TR; }
+};
+
+// Whether queries at p0 .. p1 see all of, or anything of, the keys j0 .. j0 + width - 1.
+__device__ __forceinline__ bool sees_all(const WindowArgs& a, int k_len, int p0, int p1, int j0, int width) {
+  const int last = j0 + width - 1;
+  return last < k_len && last <= p0 && (j0 > p1 - a.window || last < a.sinks);
+}
+__device__ __forceinline__ bool sees_any(const WindowArgs& a, int k_len, int p0, int p1, int j0, int width) {
+  return j0 < k_len && j0 <= p1 && (j0 + width - 1 > p0 - a.window || j0 < a.sinks);
+}
+
+// Loads of a wave's share of a 64-row tile, 1 KB segments of RPI rows.  A lane's 16 bytes of segment i lie at its row (lane / NCH, from the segment's
+// first) and at the chunk that the swizzle puts there, of which there are OFFS different ones: those offsets are kept, the segment's first
+// row goes into the uniform base.  Of a tile with fewer than 64 rows (at least one) the last row is loaded again.
+template <int DH, int WAVES, bool SWZ16>
+struct TileLoads {
+  static constexpr int NCH = DH / 8, RPI = 64 / NCH, NSEG = DH / 8 / WAVES, OFFS = RPI == 8 ? 1 : 16 / RPI < NSEG ? 16 / RPI : NSEG;
+  unsigned off[OFFS];
+  int wave, ld;
+  __device__ __forceinline__ static int chunk_of(int row) {
+    return ((threadIdx.x & 63) % NCH) ^ (SWZ16 ? swz16(row) : swz<DH>(row));
+  }
+  __device__ __forceinline__ TileLoads(int wave_, long long ld_) {
+    wave = wave_;
+    ld = (int)ld_;
+    const int r = (threadIdx.x & 63) / NCH;
+#pragma unroll
+    for (int i = 0; i < OFFS; i++) off[i] = (unsigned)(r * ld) * 2u + chunk_of((wave * NSEG + i) * RPI + r) * 16u;
+  }
+  __device__ __forceinline__ void segment(const bf16_t* tile, int rows, unsigned lds_tile, int i) const {
+    const int first = (wave * NSEG + i) * RPI;
+    const unsigned dst = __builtin_amdgcn_readfirstlane(lds_tile + (wave * NSEG + i) * 1024u);
+    if (rows >= TR) {
+      lds_dma16(tile + (long long)first * ld, off[i % OFFS], dst);
+    } else {
+      const int row = first + (threadIdx.x & 63) / NCH;
+      lds_dma16(tile, (unsigned)(min(row, rows - 1) * ld) * 2u + chunk_of(row) * 16u, dst);
+    }
+  }
+};
+// Whether this lane's chunk of segment i lies within the head (masked-edge form).
+template <int DH, int WAVES, bool SWZ16>
+__device__ __forceinline__ bool lane_in_head(int wave, int i, int chunks) {
+  constexpr int NCH = DH / 8, RPI = 64 / NCH, NSEG = DH / 8 / WAVES;
+  const int lane = threadIdx.x & 63;
+  const int row = (wave * NSEG + i) * RPI + lane / NCH;
+  return ((lane % NCH) ^ (SWZ16 ? swz16(row) : swz<DH>(row))) < chunks;
+}
+
+// The rows that a workgroup of the forward pass or of dQ has, and what it streams for them.
+template <int WPG>
+struct RowTile {
+  int b, hk, r0, rows;       // key head; first row of the workgroup, rows of the key head
+  int wave, row, i, h, p;    // this lane's row: query, query head, position
+  bool ok;                   // there is such a row
+  int p0, p1, wp0, wp1;      // positions of the workgroup's rows, of the wave's
+  __device__ __forceinline__ RowTile(const WindowArgs& a, const WindowSeq& s, int b_, int hk_, int tile) {
+    b = b_; hk = hk_;
+    rows = a.Sq * a.group;
+    r0 = tile * (32 * WPG);
+    wave = WPG == 1 ? 0 : __builtin_amdgcn_readfirstlane(threadIdx.x >> 6);
+    const int w0 = r0 + wave * 32;
+    row = w0 + (threadIdx.x & 31);
+    ok = row < rows;
+    const int r = min(row, rows - 1);
+    i = r / a.group;
+    h = hk * a.group + r - i * a.group;
+    p = s.pos0 + i;
+    p0 = s.pos0 + r0 / a.group;
+    p1 = s.pos0 + min(r0 + 32 * WPG - 1, rows - 1) / a.group;
+    wp0 = s.pos0 + min(w0, rows - 1) / a.group;
+    wp1 = w0 < rows ? s.pos0 + min(w0 + 31, rows - 1) / a.group : -2147483647 - 1;  // (a wave without rows sees nothing)
+  }
+};
+
+// dK and dV.  A workgroup has a tile of keys of one key head and streams the 64-query tiles of all its query heads that see some of
+// them, head by head.  Keys among the sinks are seen by every later query, not by a window's length of them: their tiles' streams are cut into
+// `splits` parts, workgroups of their own that leave sums for window_fold_kernel.  They are the first workgroups of the launch; the other
+// tiles follow.
+struct KeyGrid {
+  int n_tiles, sink_tiles, splits, sink_blocks;  // key tiles of a head; how many of them are split, into how many parts; workgroups of those
+};
+struct KeyItem {
+  int bh, tile, split;  // split < 0: whole
+  bool ok;
+  __device__ __forceinline__ KeyItem(const KeyGrid& k, int heads, int block, int grid) {
+    if (block < k.sink_blocks) {
+      split = block % k.splits;
+      const int r = block / k.splits;
+      tile = r % max(k.sink_tiles, 1);
+      bh = r / max(k.sink_tiles, 1);
+      ok = bh < heads;
+    } else {
+      const int rest = k.n_tiles - k.sink_tiles, i = xcd_item(block - k.sink_blocks, grid - k.sink_blocks);
+      split = -1;
+      ok = i < rest * heads;
+      tile = k.sink_tiles + i % max(rest, 1);
+      bh = i / max(rest, 1);
+    }
+  }
+};
+
+}  // namespace fax
