@@ -102,7 +102,7 @@ __global__ __launch_bounds__(64 * WPG, 2) void window_dkv_mfma_kernel(WindowArgs
   // queries that see this lane's key
   const QueryRange mine(a, sq, jk, jk + 1);
   const f32x16 zero = {0.f, 0.f, 0.f, 0.f, 0.f, 0.f, 0.f, 0.f, 0.f, 0.f, 0.f, 0.f, 0.f, 0.f, 0.f, 0.f};
-  auto tile = [&](auto mask_c, int i0, int buf) {
+  auto tile = [&](auto mask_c, int i0, int buf) __attribute__((always_inline)) {
     constexpr bool MASK = decltype(mask_c)::value;
     int lane_t = lane;
     settle(lane_t);  // fragment addresses are formed tile by tile: kept from tile to tile they are some thirty registers
@@ -163,17 +163,40 @@ __global__ __launch_bounds__(64 * WPG, 2) void window_dkv_mfma_kernel(WindowArgs
     qs.load(u0, 0);
     lds_dma_wait();
     __syncthreads();
-    for (int u = u0; u < u1; u++) {
-      const int i0 = qs.query(u), buf = (u - u0) & 1, rows = a.Sq - i0;
-      if (u + 1 < u1) qs.load(u + 1, buf ^ 1);
-      const int p0 = sq.pos0 + i0, p1 = p0 + min(TR, rows) - 1;
-      if (rows >= TR && sees_all(a, sq.k_len, p0, p1, j0w, 32)) {
-        tile(F_{}, i0, buf);
-      } else if (sees_any(a, sq.k_len, p0, p1, j0w, 32)) {
-        tile(T_{}, i0, buf);
-      }
+    // Runs of tiles with and without masks in loops of their own, as in the forward pass.
+    auto positions = [&](int u, int& p0, int& p1) __attribute__((always_inline)) {
+      const int i0 = qs.query(u);
+      p0 = sq.pos0 + i0;
+      p1 = p0 + min(TR, a.Sq - i0) - 1;
+    };
+    auto full = [&](int u) __attribute__((always_inline)) {
+      int p0, p1;
+      positions(u, p0, p1);
+      return p1 - p0 == TR - 1 && sees_all(a, sq.k_len, p0, p1, j0w, 32);
+    };
+    auto any = [&](int u) __attribute__((always_inline)) {
+      int p0, p1;
+      positions(u, p0, p1);
+      return sees_any(a, sq.k_len, p0, p1, j0w, 32);
+    };
+    auto next = [&](int u) __attribute__((always_inline)) {
+      if (u + 1 < u1) qs.load(u + 1, (u - u0 + 1) & 1);
+    };
+    auto done = [&]() __attribute__((always_inline)) {
       lds_dma_wait();
       __syncthreads();
+    };
+    for (int u = u0; u < u1;) {
+      for (; u < u1 && !full(u); u++) {
+        next(u);
+        if (any(u)) tile(T_{}, qs.query(u), (u - u0) & 1);
+        done();
+      }
+      for (; u < u1 && full(u); u++) {
+        next(u);
+        tile(F_{}, qs.query(u), (u - u0) & 1);
+        done();
+      }
     }
   }
 
@@ -249,7 +272,7 @@ __global__ __launch_bounds__(64 * WPG, 2) void window_dkv16_mfma_kernel(WindowAr
     for (int r = 0; r < 4; r++) dk[dt][r] = dv[dt][r] = 0.f;
   const QueryRange mine(a, sq, jk, jk + 1);
   const f32x4 zero = {0.f, 0.f, 0.f, 0.f};
-  auto tile = [&](auto mask_c, int i0, int buf) {
+  auto tile = [&](auto mask_c, int i0, int buf) __attribute__((always_inline)) {
     constexpr bool MASK = decltype(mask_c)::value;
     int lane_t = lane;
     settle(lane_t);  // fragment addresses are formed tile by tile: kept from tile to tile they are some thirty registers
@@ -312,17 +335,40 @@ __global__ __launch_bounds__(64 * WPG, 2) void window_dkv16_mfma_kernel(WindowAr
     qs.load(u0, 0);
     lds_dma_wait();
     __syncthreads();
-    for (int u = u0; u < u1; u++) {
-      const int i0 = qs.query(u), buf = (u - u0) & 1, rows = a.Sq - i0;
-      if (u + 1 < u1) qs.load(u + 1, buf ^ 1);
-      const int p0 = sq.pos0 + i0, p1 = p0 + min(TR, rows) - 1;
-      if (rows >= TR && sees_all(a, sq.k_len, p0, p1, j0w, 16)) {
-        tile(F_{}, i0, buf);
-      } else if (sees_any(a, sq.k_len, p0, p1, j0w, 16)) {
-        tile(T_{}, i0, buf);
-      }
+    // Runs of tiles with and without masks in loops of their own, as in the forward pass.
+    auto positions = [&](int u, int& p0, int& p1) __attribute__((always_inline)) {
+      const int i0 = qs.query(u);
+      p0 = sq.pos0 + i0;
+      p1 = p0 + min(TR, a.Sq - i0) - 1;
+    };
+    auto full = [&](int u) __attribute__((always_inline)) {
+      int p0, p1;
+      positions(u, p0, p1);
+      return p1 - p0 == TR - 1 && sees_all(a, sq.k_len, p0, p1, j0w, 16);
+    };
+    auto any = [&](int u) __attribute__((always_inline)) {
+      int p0, p1;
+      positions(u, p0, p1);
+      return sees_any(a, sq.k_len, p0, p1, j0w, 16);
+    };
+    auto next = [&](int u) __attribute__((always_inline)) {
+      if (u + 1 < u1) qs.load(u + 1, (u - u0 + 1) & 1);
+    };
+    auto done = [&]() __attribute__((always_inline)) {
       lds_dma_wait();
       __syncthreads();
+    };
+    for (int u = u0; u < u1;) {
+      for (; u < u1 && !full(u); u++) {
+        next(u);
+        if (any(u)) tile(T_{}, qs.query(u), (u - u0) & 1);
+        done();
+      }
+      for (; u < u1 && full(u); u++) {
+        next(u);
+        tile(F_{}, qs.query(u), (u - u0) & 1);
+        done();
+      }
     }
   }
 

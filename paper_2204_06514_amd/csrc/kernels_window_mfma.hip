@@ -54,7 +54,7 @@ __global__ __launch_bounds__(64 * WPG, 2) void window_fwd_mfma_kernel(WindowArgs
   bool in_head[NSEG];
 #pragma unroll
   for (int i = 0; i < NSEG; i++) in_head[i] = !EDGE || lane_in_head<DH, WPG, false>(wave, i, nch);
-  auto load = [&](int j0, int buf) {
+  auto load = [&](int j0, int buf) __attribute__((always_inline)) {
     const long long at = (long long)j0 * a.skv.row;
 #pragma unroll
     for (int i = 0; i < NSEG; i++)
@@ -64,7 +64,7 @@ __global__ __launch_bounds__(64 * WPG, 2) void window_fwd_mfma_kernel(WindowArgs
       }
   };
   const int p = rt.p, last = min(p, sq.k_len - 1), first = p - a.window;  // sees keys in (first, last] and the sinks up to last
-  auto tile = [&](auto mask_c, int j0, int buf) {
+  auto tile = [&](auto mask_c, int j0, int buf) __attribute__((always_inline)) {
     constexpr bool MASK = decltype(mask_c)::value;
     int lane_t = lane;
     settle(lane_t);  // fragment addresses are formed tile by tile: kept from tile to tile they are some thirty registers
@@ -144,16 +144,27 @@ __global__ __launch_bounds__(64 * WPG, 2) void window_fwd_mfma_kernel(WindowArgs
     load(kt.key(u0), 0);
     lds_dma_wait();
     __syncthreads();
-    for (int u = u0; u < u1; u++) {
-      const int j0 = kt.key(u), buf = (u - u0) & 1;
-      if (u + 1 < u1) load(kt.key(u + 1), buf ^ 1);
-      if (sees_all(a, sq.k_len, rt.wp0, rt.wp1, j0, TR)) {
-        tile(F_{}, j0, buf);
-      } else if (sees_any(a, sq.k_len, rt.wp0, rt.wp1, j0, TR)) {
-        tile(T_{}, j0, buf);
-      }
+    // Runs of tiles that take the masks (or that no row of the wave sees) and of tiles that do not, in loops of their own: one loop over both kinds
+    // keeps the accumulators in two places, which does not fit the registers.
+    auto full = [&](int u) { return sees_all(a, sq.k_len, rt.wp0, rt.wp1, kt.key(u), TR); };
+    auto next = [&](int u) __attribute__((always_inline)) {
+      if (u + 1 < u1) load(kt.key(u + 1), (u - u0 + 1) & 1);
+    };
+    auto done = [&]() {
       lds_dma_wait();
       __syncthreads();
+    };
+    for (int u = u0; u < u1;) {
+      for (; u < u1 && !full(u); u++) {
+        next(u);
+        if (sees_any(a, sq.k_len, rt.wp0, rt.wp1, kt.key(u), TR)) tile(T_{}, kt.key(u), (u - u0) & 1);
+        done();
+      }
+      for (; u < u1 && full(u); u++) {
+        next(u);
+        tile(F_{}, kt.key(u), (u - u0) & 1);
+        done();
+      }
     }
   }
 
@@ -243,7 +254,7 @@ __global__ __launch_bounds__(64 * WPG, 2) void window_dq_mfma_kernel(WindowArgs 
   bool in_head[NSEG];
 #pragma unroll
   for (int i = 0; i < NSEG; i++) in_head[i] = !EDGE || lane_in_head<DH, WPG, false>(wave, i, nch);
-  auto load = [&](int j0, int buf) {
+  auto load = [&](int j0, int buf) __attribute__((always_inline)) {
     const long long at = (long long)j0 * a.skv.row;
 #pragma unroll
     for (int i = 0; i < NSEG; i++)
@@ -254,7 +265,7 @@ __global__ __launch_bounds__(64 * WPG, 2) void window_dq_mfma_kernel(WindowArgs 
   };
   const f32x16 zero = {0.f, 0.f, 0.f, 0.f, 0.f, 0.f, 0.f, 0.f, 0.f, 0.f, 0.f, 0.f, 0.f, 0.f, 0.f, 0.f};
   const int p = rt.p, last = min(p, sq.k_len - 1), first = p - a.window;
-  auto tile = [&](auto mask_c, int j0, int buf) {
+  auto tile = [&](auto mask_c, int j0, int buf) __attribute__((always_inline)) {
     constexpr bool MASK = decltype(mask_c)::value;
     int lane_t = lane;
     settle(lane_t);  // fragment addresses are formed tile by tile: kept from tile to tile they are some thirty registers
@@ -305,16 +316,27 @@ __global__ __launch_bounds__(64 * WPG, 2) void window_dq_mfma_kernel(WindowArgs 
     load(kt.key(0), 0);
     lds_dma_wait();
     __syncthreads();
-    for (int u = 0; u < kt.n; u++) {
-      const int j0 = kt.key(u), buf = u & 1;
-      if (u + 1 < kt.n) load(kt.key(u + 1), buf ^ 1);
-      if (sees_all(a, sq.k_len, rt.wp0, rt.wp1, j0, TR)) {
-        tile(F_{}, j0, buf);
-      } else if (sees_any(a, sq.k_len, rt.wp0, rt.wp1, j0, TR)) {
-        tile(T_{}, j0, buf);
-      }
+    // Runs of tiles that take the masks (or that no row of the wave sees) and of tiles that do not, in loops of their own: one loop over both kinds
+    // keeps the accumulators in two places, which does not fit the registers.
+    auto full = [&](int u) { return sees_all(a, sq.k_len, rt.wp0, rt.wp1, kt.key(u), TR); };
+    auto next = [&](int u) __attribute__((always_inline)) {
+      if (u + 1 < kt.n) load(kt.key(u + 1), (u + 1) & 1);
+    };
+    auto done = [&]() {
       lds_dma_wait();
       __syncthreads();
+    };
+    for (int u = 0; u < kt.n;) {
+      for (; u < kt.n && !full(u); u++) {
+        next(u);
+        if (sees_any(a, sq.k_len, rt.wp0, rt.wp1, kt.key(u), TR)) tile(T_{}, kt.key(u), (u) & 1);
+        done();
+      }
+      for (; u < kt.n && full(u); u++) {
+        next(u);
+        tile(F_{}, kt.key(u), (u) & 1);
+        done();
+      }
     }
   }
   const unsigned long long odd = __builtin_amdgcn_ballot_w64(rt.ok && not_finite(dq, 0.f) != 0.f);

@@ -38,6 +38,13 @@ __device__ __forceinline__ bool sees_any(const WindowArgs& a, int k_len, int p0,
   return j0 < k_len && j0 <= p1 && (j0 + width - 1 > p0 - a.window || j0 < a.sinks);
 }
 
+// The same address for the whole wave, in scalar registers, whatever the compiler keeps it in.
+__device__ __forceinline__ const bf16_t* uniform(const bf16_t* p) {
+  const unsigned long long v = (unsigned long long)p;
+  const unsigned lo = __builtin_amdgcn_readfirstlane((unsigned)v), hi = __builtin_amdgcn_readfirstlane((unsigned)(v >> 32));
+  return (const bf16_t*)(((unsigned long long)hi << 32) | lo);
+}
+
 // Loads of a wave's share of a 64-row tile, 1 KB segments of RPI rows.  A lane's 16 bytes of segment i lie at its row (lane / NCH, from the segment's
 // first) and at the chunk that the swizzle puts there, of which there are OFFS different ones: those offsets are kept, the segment's first
 // row goes into the uniform base.  Of a tile with fewer than 64 rows (at least one) the last row is loaded again.
@@ -60,10 +67,10 @@ struct TileLoads {
     const int first = (wave * NSEG + i) * RPI;
     const unsigned dst = __builtin_amdgcn_readfirstlane(lds_tile + (wave * NSEG + i) * 1024u);
     if (rows >= TR) {
-      lds_dma16(tile + (long long)first * ld, off[i % OFFS], dst);
+      lds_dma16(uniform(tile + (long long)first * ld), off[i % OFFS], dst);
     } else {
       const int row = first + (threadIdx.x & 63) / NCH;
-      lds_dma16(tile, (unsigned)(min(row, rows - 1) * ld) * 2u + chunk_of(row) * 16u, dst);
+      lds_dma16(uniform(tile), (unsigned)(min(row, rows - 1) * ld) * 2u + chunk_of(row) * 16u, dst);
     }
   }
 };
