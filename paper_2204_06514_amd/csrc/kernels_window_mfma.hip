@@ -118,14 +118,21 @@ __global__ __launch_bounds__(64 * WPG, 2) void window_fwd_mfma_kernel(WindowArgs
     }
     const float mc = m * c;
     float rs = 0.f;
-    bf16x8 pb[2][2];  // probabilities as the second product's factors: bf16, half a step (2^-8) off each; the denominator adds them unrounded
+    // Probabilities as the second product's factors: bf16, half a step (2^-8) off each (the denominator adds them unrounded), which leaves ctx 1.4 times as
+    // far off as its own rounding.  PART, bound by memory: two bf16 numbers, and ctx as good as its rounding.
+    bf16x8 pb[2][2], pl[2][2];
 #pragma unroll
     for (int jt = 0; jt < 2; jt++)
 #pragma unroll
       for (int v = 0; v < 16; v++) {
         const float e = __builtin_amdgcn_exp2f(fmaf(s[jt][v], c, -mc));
         rs += e;
-        pb[jt][v >> 3][v & 7] = (__bf16)e;
+        if (PART) {
+          s[jt][v] = e;
+          if (v & 1) split2(s[jt][v - 1], e, pb[jt][v >> 3], pl[jt][v >> 3], (v & 7) >> 1);
+        } else {
+          pb[jt][v >> 3][v & 7] = (__bf16)e;
+        }
       }
     l += sum32(rs);
     __builtin_amdgcn_sched_barrier(0);
@@ -134,6 +141,7 @@ __global__ __launch_bounds__(64 * WPG, 2) void window_fwd_mfma_kernel(WindowArgs
     for (int i = 0; i < N; i++) {
       const int dt = i % DT, ch = i / DT;
       oacc[dt] = __builtin_amdgcn_mfma_f32_32x32x16_bf16(fc[i % LEAD], pb[ch % 2][ch / 2], oacc[dt], 0, 0, 0);
+      if (PART) oacc[dt] = __builtin_amdgcn_mfma_f32_32x32x16_bf16(fc[i % LEAD], pl[ch % 2][ch / 2], oacc[dt], 0, 0, 0);
       if (i + LEAD < N) fc[i % LEAD] = col_frag(i + LEAD);
       __builtin_amdgcn_sched_barrier(0);
     }
@@ -240,7 +248,6 @@ __global__ __launch_bounds__(64 * WPG, 2) void window_dq_mfma_kernel(WindowArgs 
     for (int e = 0; e < 8; e++) di = fmaf((float)o[e], (float)dof[ks][e], di);
   }
   di = sum32(di);
-  if (g == 0 && rt.ok) a.delta[stat] = di;
 #pragma unroll
   for (int ks = 0; ks < KS; ks++) { settle(qf[ks]); settle(dof[ks]); }
   settle(li); settle(di);
@@ -249,6 +256,7 @@ __global__ __launch_bounds__(64 * WPG, 2) void window_dq_mfma_kernel(WindowArgs 
   for (int dt = 0; dt < DT; dt++)
 #pragma unroll
     for (int v = 0; v < 16; v++) dq[dt][v] = 0.f;
+  float ds_sum = 0.f;
 
   const TileLoads<DH, WPG, false> loads(wave, a.skv.row);
   bool in_head[NSEG];
@@ -290,7 +298,7 @@ __global__ __launch_bounds__(64 * WPG, 2) void window_dq_mfma_kernel(WindowArgs 
         else f[i % LEAD] = col_frag(jt, i + LEAD - N1);
         __builtin_amdgcn_sched_barrier(0);
       }
-      bf16x8 db[2];  // dS as the second product's factor: bf16, half a step off
+      bf16x8 db[2], dl[2];  // dS as the second product's factor: two bf16 numbers, the second what the first leaves
       __builtin_amdgcn_s_setprio(0);
 #pragma unroll
       for (int v = 0; v < 16; v++) {
@@ -298,14 +306,17 @@ __global__ __launch_bounds__(64 * WPG, 2) void window_dq_mfma_kernel(WindowArgs 
         float d = e * (dp[v] - di);
         const int key = j0 + jt * 32 + (v >> 2) * 8 + g * 4 + (v & 3);
         if (MASK) d = (key > last) | ((key <= first) & (key >= a.sinks)) ? 0.f : d;
-        db[v >> 3][v & 7] = (__bf16)d;
+        ds_sum += d;
+        dp[v] = d;
+        if (v & 1) split2(dp[v - 1], d, db[v >> 3], dl[v >> 3], (v & 7) >> 1);
       }
       __builtin_amdgcn_sched_barrier(0);
       __builtin_amdgcn_s_setprio(1);
 #pragma unroll
-      for (int i = 0; i < N3; i++) {
-        dq[i % DT] = __builtin_amdgcn_mfma_f32_32x32x16_bf16(f[i % LEAD], db[i / DT], dq[i % DT], 0, 0, 0);
-        if (jt == 0) f[i % LEAD] = row_frag(1, i);
+      for (int i = 0; i < 2 * N3; i++) {  // per k-step all of the first, then all of the second: products on one accumulator stand DT apart
+        const int k = i / (2 * DT), n = k * DT + i % DT;
+        dq[i % DT] = __builtin_amdgcn_mfma_f32_32x32x16_bf16(f[n], i / DT % 2 ? dl[k] : db[k], dq[i % DT], 0, 0, 0);
+        if (jt == 0 && i / DT % 2) f[n] = row_frag(1, n);
         __builtin_amdgcn_sched_barrier(0);
       }
     }
@@ -339,6 +350,9 @@ __global__ __launch_bounds__(64 * WPG, 2) void window_dq_mfma_kernel(WindowArgs 
       }
     }
   }
+  // The probabilities of a row add up to one, so the sum of its dS is what delta, formed from ctx as it was rounded, lacks: dK gets it with that.
+  di += sum32(ds_sum);
+  if (g == 0 && rt.ok) a.delta[stat] = di;
   const unsigned long long odd = __builtin_amdgcn_ballot_w64(rt.ok && not_finite(dq, 0.f) != 0.f);
   unsigned again = (unsigned)odd | (unsigned)(odd >> 32);
   if (rt.ok && !((again >> (lane & 31)) & 1)) store_rows<DW, EDGE>(strided_row((bf16_t*)a.dq, a.sq, b, rt.i, rt.h), dq, scale, g, hw);

@@ -83,6 +83,17 @@ __device__ __forceinline__ bool lane_in_head(int wave, int i, int chunks) {
   return ((lane % NCH) ^ (SWZ16 ? swz16(row) : swz<DH>(row))) < chunks;
 }
 
+// x and y as bf16 pairs: elements 2 n and 2 n + 1 of hi cut off (not rounded), of lo what that leaves, rounded: 2^-16 off each instead of 2^-8.
+__device__ __forceinline__ void split2(float x, float y, bf16x8& hi, bf16x8& lo, int n) {
+  typedef __attribute__((ext_vector_type(4))) unsigned u4;
+  const unsigned a = __float_as_uint(x), b = __float_as_uint(y);
+  u4 h = __builtin_bit_cast(u4, hi);
+  h[n] = __builtin_amdgcn_perm(b, a, 0x07060302u);  // upper halves
+  hi = __builtin_bit_cast(bf16x8, h);
+  lo[2 * n] = (__bf16)(x - __uint_as_float(a & 0xffff0000u));
+  lo[2 * n + 1] = (__bf16)(y - __uint_as_float(b & 0xffff0000u));
+}
+
 // The rows that a workgroup of the forward pass or of dQ has, and what it streams for them.
 template <int WPG>
 struct RowTile {
