@@ -1,44 +1,77 @@
-// Embedding lookup with scaling, and its gradient by sorted tokens.
-//
-// Gradient.  dtable[v] = scale * sum of dout[n] over the positions n that hold id v.  Positions are sorted by id (stably: ascending
-// within an id), then every row of dtable has one writer that adds its positions' rows in order: no atomics, the same bits every time.
-//   sort     least significant digit first, of SORT_BITS bits at most.  A wave has a run of consecutive positions and ranks 64 at a time by
-//            comparing their digits bit by bit (ballots); ranks across waves come from a table of counts by digit and wave, scanned in that order.
-//   chunks   of CHUNK sorted positions that all hold the same id are added up into a row of scratch each, so that a frequent id, of which a
-//            text has thousands, is not one workgroup's chain.
-//   rows     one workgroup to a row: what comes before the first whole chunk, the chunks' sums, what comes after the last.
-// Ids outside [0, V) sort behind all others and are not looked at again.
+// Embedding lookup with scaling, and its gradient by sorted tokens.  Both are bound by memory.
+#include <type_traits>
+
 #include "fax_internal.h"
 
 namespace fax {
 
+// x / d for x < 2^31 as a multiplication, d >= 1: q = (x * m) >> s with m = ceil(2^s / d), s = 31 + ceil(log2 d) (Granlund and Montgomery, 1994);
+// m is at most 2^32 + 1, the product fits 64 bits.
+struct Divider {
+  uint64_t m;
+  unsigned s, d;
+  explicit Divider(unsigned d_) : d(d_) {
+    unsigned l = 0;
+    while ((1ull << l) < d) l++;
+    s = 31 + l;
+    m = ((1ull << s) + d - 1) / d;
+  }
+  __device__ __forceinline__ unsigned operator()(unsigned x) const { return (unsigned)((x * m) >> s); }
+};
+
 // ---- lookup -----------------------------------------------------------------------------------------
-template <typename T>
-__global__ __launch_bounds__(256) void embedding_fwd_kernel(int N, int V, int D, const int32_t* __restrict__ tokens, const T* __restrict__ table,
-                                                            float scale, T* __restrict__ out) {
-  constexpr int E = Vec16<T>::N;
-  for (int n = blockIdx.x; n < N; n += gridDim.x) {
-    const int id = tokens[n];
-    const bool known = id >= 0 && id < V;
-    const T* row = table + (size_t)(known ? id : 0) * D;
-    T* o = out + (size_t)n * D;
-    if (D % E == 0) {
-      for (int d = threadIdx.x * E; d < D; d += 256 * E) {
-        Vec16<T> x;
-        x.load(row + d);
+// A thread has LOOKUPS vectors of the output, 256 apart: their ids, then their rows' vectors are in flight together.  (A workgroup to a row, with a
+// thread to a vector, leaves most of 256 threads idle at common widths.)
+static constexpr int LOOKUPS = 4;
+template <typename T, int E>
+__global__ __launch_bounds__(256) void embedding_fwd_kernel(unsigned first_row, unsigned vectors, Divider per_row, int V, int D, const int32_t* __restrict__ tokens,
+                                                            const T* __restrict__ table, float scale, T* __restrict__ out) {
+  const unsigned base = blockIdx.x * (256u * LOOKUPS) + threadIdx.x;
+  int id[LOOKUPS];
+  unsigned col[LOOKUPS];
+  tokens += first_row;
+  out += (size_t)first_row * D;
 #pragma unroll
-        for (int k = 0; k < E; k++) x.set(k, known ? x.get(k) * scale : 0.f);
-        x.store(o + d);
-      }
-    } else {
-      for (int d = threadIdx.x; d < D; d += 256) o[d] = from_f<T>(known ? to_f(row[d]) * scale : 0.f);
+  for (int k = 0; k < LOOKUPS; k++) {
+    const unsigned x = base + 256u * k;
+    const unsigned row = x < vectors ? per_row(x) : 0;
+    col[k] = x - row * per_row.d;
+    id[k] = x < vectors ? tokens[row] : -1;
+  }
+  if constexpr (E == 1) {
+#pragma unroll
+    for (int k = 0; k < LOOKUPS; k++) {
+      const unsigned x = base + 256u * k;
+      if (x < vectors) out[x] = from_f<T>(id[k] >= 0 && id[k] < V ? to_f(table[(size_t)id[k] * D + col[k]]) * scale : 0.f);
+    }
+  } else {
+    Vec16<T> v[LOOKUPS];
+#pragma unroll
+    for (int k = 0; k < LOOKUPS; k++)
+      if (id[k] >= 0 && id[k] < V) v[k].load(table + (size_t)id[k] * D + col[k] * E);
+#pragma unroll
+    for (int k = 0; k < LOOKUPS; k++) {
+      const unsigned x = base + 256u * k;
+      if (x >= vectors) continue;
+      const bool known = id[k] >= 0 && id[k] < V;
+      Vec16<T> o;
+#pragma unroll
+      for (int e = 0; e < E; e++) o.set(e, known ? v[k].get(e) * scale : 0.f);
+      o.store_nt(out + (size_t)x * E);
     }
   }
 }
 
-template <typename T>
+template <typename T, int E>
 static int embedding_fwd_t(int N, int V, int D, const int32_t* tokens, const T* table, float scale, T* out, hipStream_t s) {
-  hipLaunchKernelGGL(embedding_fwd_kernel<T>, dim3(N), dim3(256), 0, s, N, V, D, tokens, table, scale, out);
+  const unsigned per_row = D / E;
+  const Divider div(per_row);
+  const int rows = (int)(0x7fffffffu / per_row) < N ? (int)(0x7fffffffu / per_row) : N;  // of a launch: vectors count in 31 bits
+  for (int r = 0; r < N; r += rows) {
+    const unsigned vectors = (unsigned)(N - r < rows ? N - r : rows) * per_row;
+    const unsigned blocks = (unsigned)(((uint64_t)vectors + 256 * LOOKUPS - 1) / (256 * LOOKUPS));
+    hipLaunchKernelGGL((embedding_fwd_kernel<T, E>), dim3(blocks), dim3(256), 0, s, (unsigned)r, vectors, div, V, D, tokens, table, scale, out);
+  }
   FAX_LAUNCH_CHECK("embedding_fwd");
   return FAX_OK;
 }
@@ -46,31 +79,51 @@ static int embedding_fwd_t(int N, int V, int D, const int32_t* tokens, const T* 
 int embedding_fwd(int dtype, int N, int V, int D, const int32_t* tokens, const void* table, float scale, void* out, hipStream_t s) {
   if (N == 0) return FAX_OK;
   Timed t_("embedding_fwd", WORK_BYTE, 2.0 * N * D * (dtype == FAX_F32 ? 4.0 : 2.0) + 4.0 * N, s);
-  if (dtype == FAX_F32) return embedding_fwd_t<float>(N, V, D, tokens, (const float*)table, scale, (float*)out, s);
-  return embedding_fwd_t<bf16_t>(N, V, D, tokens, (const bf16_t*)table, scale, (bf16_t*)out, s);
+  if (dtype == FAX_F32)
+    return D % 4 == 0 ? embedding_fwd_t<float, 4>(N, V, D, tokens, (const float*)table, scale, (float*)out, s)
+                      : embedding_fwd_t<float, 1>(N, V, D, tokens, (const float*)table, scale, (float*)out, s);
+  return D % 8 == 0 ? embedding_fwd_t<bf16_t, 8>(N, V, D, tokens, (const bf16_t*)table, scale, (bf16_t*)out, s)
+                    : embedding_fwd_t<bf16_t, 1>(N, V, D, tokens, (const bf16_t*)table, scale, (bf16_t*)out, s);
 }
 
-// ---- sorting positions by id ------------------------------------------------------------------------
-static constexpr int SORT_BITS = 9, BINS = 1 << SORT_BITS;
-static constexpr int WAVE_KEYS = 1024;  // positions of a wave, where there are enough of them
+// ---- gradient ---------------------------------------------------------------------------------------
+// dtable[v] = scale * sum of dout[n] over the positions n that hold id v.  Positions are sorted by id (stably: ascending within an
+// id), then every row of dtable has one writer that adds its positions' rows in an order that depends on the ids alone: no floating-point
+// atomics, the same bits every time.
+//   sort    least significant digit first.  A workgroup has a run of consecutive positions.  A table of counts by run and digit gives where each run's
+//           keys of a digit begin (every workgroup adds up what it needs of it); within a run, 64 keys at a time are ranked by comparing their digits bit
+//           by bit (ballots).
+//   chunks  of CHUNK sorted positions that all hold the same id are added up into a row of scratch each, so that a frequent id, of which a text has
+//           thousands, is not one wavefront's chain.
+//   rows    one wavefront to ROWS rows of dtable.  Rows with whole chunks have a workgroup each: what comes before the first, the chunks' sums in four
+//           parts, what comes after the last.
+// Up to DIRECT positions there is no sort: a wavefront finds a row's positions among all of them.
+// Ids outside [0, V) sort behind all others and are not looked at again.
+static constexpr int SORT_BITS = 8, BINS = 1 << SORT_BITS;
+static constexpr int RUN_KEYS = 1024;  // positions of a run, where that leaves at most MOST_RUNS
+static constexpr int MOST_RUNS = 256;
+static constexpr int SMALL_KEYS = 4096;  // up to here one workgroup sorts in LDS
+static constexpr int DIRECT = 512;
 static constexpr int CHUNK = 32;
+static constexpr int ROWS = 4;
 
 struct SortPlan {
   int bits, passes;   // of a digit, digits
-  int per_wave, waves;
+  int run_keys, runs;
 };
 static SortPlan sort_plan(int N, int V) {
   SortPlan p;
   int bits = 1;
-  while (bits < 31 && (V >> bits) != 0) bits++;  // ids 0 .. V
+  while (bits < 31 && (V >> bits) != 0) bits++;  // keys 0 .. V
   p.passes = (bits + SORT_BITS - 1) / SORT_BITS;
   p.bits = (bits + p.passes - 1) / p.passes;
-  p.per_wave = WAVE_KEYS;
-  p.waves = (N + WAVE_KEYS - 1) / WAVE_KEYS;
+  p.run_keys = RUN_KEYS;
+  if (N > RUN_KEYS * MOST_RUNS) p.run_keys = ((N + MOST_RUNS - 1) / MOST_RUNS + RUN_KEYS - 1) / RUN_KEYS * RUN_KEYS;
+  p.runs = (N + p.run_keys - 1) / p.run_keys;
   return p;
 }
 
-// Digit of lane's key, the lanes that have the same one, and this lane's place among them.  Lanes without a key (ok false) match nobody.
+// The lanes that have the same digit as this one.  Lanes without a key (ok false) match nobody.
 __device__ __forceinline__ unsigned long long same_digit(unsigned digit, int bits, bool ok) {
   unsigned long long m = __builtin_amdgcn_ballot_w64(ok);
   for (int b = 0; b < bits; b++) {
@@ -84,127 +137,249 @@ __device__ __forceinline__ int below(unsigned long long m) {
 }
 __device__ __forceinline__ unsigned key_of(int id, int V) { return (unsigned)id < (unsigned)V ? (unsigned)id : (unsigned)V; }
 
-// counts[digit * waves + wave] of one pass.  in_pos NULL: the positions in order (first pass), with keys from the tokens.
-__global__ __launch_bounds__(256) void sort_count_kernel(int N, int V, int shift, int bits, int per_wave, int waves, const int32_t* __restrict__ tokens,
-                                                         const uint32_t* __restrict__ in_key, uint32_t* __restrict__ counts) {
-  __shared__ unsigned hist[4][BINS];
-  const int wave = threadIdx.x >> 6, lane = threadIdx.x & 63, w = blockIdx.x * 4 + wave;
-  const unsigned bins = 1u << bits;
-  for (unsigned i = threadIdx.x; i < 4 * BINS; i += 256) (&hist[0][0])[i] = 0;
-  __syncthreads();
-  if (w < waves) {
-    const long long k0 = (long long)w * per_wave;
-    for (int k = lane; k < per_wave && k0 + k < N; k += 64) {
-      const unsigned key = in_key ? in_key[k0 + k] : key_of(tokens[k0 + k], V);
-      atomicAdd(&hist[wave][(key >> shift) & (bins - 1)], 1u);
-    }
-  }
-  __syncthreads();
-  if (w < waves)
-    for (unsigned d = lane; d < bins; d += 64) counts[(size_t)d * waves + w] = hist[wave][d];
-}
-
-// counts -> exclusive prefix sums, in place; one workgroup.
-__global__ __launch_bounds__(1024) void sort_scan_kernel(int n, uint32_t* __restrict__ counts) {
-  __shared__ unsigned sums[16];
+// One pass over a workgroup's keys: `waves` wavefronts with `per_wave` consecutive keys each (a multiple of 64).  get(k): key and position k of the run
+// (k < n); next: where each digit's next key goes, by wavefront; put(to, key, position).
+template <typename Get, typename Put>
+__device__ __forceinline__ void place_keys(int n, int per_wave, int shift, int bits, volatile unsigned* next, Get get, Put put) {
   const int lane = threadIdx.x & 63, wave = threadIdx.x >> 6;
-  unsigned carry = 0;
-  for (int base = 0; base < n; base += 1024 * 4) {
-    const int i = base + threadIdx.x * 4;
-    unsigned c[4], t = 0;
-#pragma unroll
-    for (int k = 0; k < 4; k++) {
-      c[k] = i + k < n ? counts[i + k] : 0u;
-      t += c[k];
-    }
-    unsigned inc = t;
-#pragma unroll
-    for (int o = 1; o < 64; o <<= 1) {
-      const unsigned x = __shfl_up(inc, o, 64);
-      if (lane >= o) inc += x;
-    }
-    __syncthreads();
-    if (lane == 63) sums[wave] = inc;
-    __syncthreads();
-    unsigned before = 0, total = 0;
-    for (int k = 0; k < 16; k++) {
-      if (k < wave) before += sums[k];
-      total += sums[k];
-    }
-    unsigned x = carry + before + inc - t;
-#pragma unroll
-    for (int k = 0; k < 4; k++) {
-      if (i + k < n) counts[i + k] = x;
-      x += c[k];
-    }
-    carry += total;
-  }
-}
-
-__global__ __launch_bounds__(256) void sort_place_kernel(int N, int V, int shift, int bits, int per_wave, int waves, const int32_t* __restrict__ tokens,
-                                                         const uint32_t* __restrict__ in_key, const uint32_t* __restrict__ in_pos,
-                                                         const uint32_t* __restrict__ starts, uint32_t* __restrict__ out_key, uint32_t* __restrict__ out_pos) {
-  __shared__ unsigned next_all[4][BINS];
-  const int wave = threadIdx.x >> 6, lane = threadIdx.x & 63, w = blockIdx.x * 4 + wave;
-  const unsigned bins = 1u << bits;
-  if (w >= waves) return;  // (no barrier below: a wave works on its own, its LDS operations are in order)
-  volatile unsigned* next = next_all[wave];
-  for (unsigned d = lane; d < bins; d += 64) next[d] = starts[(size_t)d * waves + w];
-  const long long k0 = (long long)w * per_wave;
-  for (int k = 0; k < per_wave && k0 + k < N; k += 64) {
-    const bool ok = k + lane < per_wave && k0 + k + lane < N;
-    const long long at = k0 + k + lane;
+  const int k0 = wave * per_wave, k1 = min(n, k0 + per_wave);
+  for (int k = k0; k < k1; k += 64) {
+    const bool ok = k + lane < k1;
     unsigned key = 0, pos = 0;
-    if (ok) {
-      key = in_key ? in_key[at] : key_of(tokens[at], V);
-      pos = in_pos ? in_pos[at] : (unsigned)at;
-    }
-    const unsigned digit = (key >> shift) & (bins - 1);
+    if (ok) get(k + lane, key, pos);
+    const unsigned digit = (key >> shift) & ((1u << bits) - 1);
     const unsigned long long m = same_digit(digit, bits, ok);
     const int rank = below(m);
     unsigned to = 0;
     if (ok) to = next[digit] + rank;
-    __builtin_amdgcn_wave_barrier();
+    __builtin_amdgcn_wave_barrier();  // (one wavefront: its LDS operations are in order)
     if (ok && rank == 0) next[digit] = to + (unsigned)__popcll(m);
     __builtin_amdgcn_wave_barrier();
-    if (ok) {
-      out_key[to] = key;
-      out_pos[to] = pos;
-    }
+    if (ok) put(to, key, pos);
+  }
+}
+
+// Exclusive prefix sums over 256 values, one to a thread of the first 256; `tmp`: 4 words of LDS.
+__device__ __forceinline__ unsigned scan256(unsigned x, unsigned* tmp) {
+  const int lane = threadIdx.x & 63, wave = threadIdx.x >> 6;
+  unsigned inc = x;
+#pragma unroll
+  for (int o = 1; o < 64; o <<= 1) {
+    const unsigned y = __shfl_up(inc, o, 64);
+    if (lane >= o) inc += y;
+  }
+  if (wave < 4 && lane == 63) tmp[wave] = inc;
+  __syncthreads();
+  unsigned before = 0;
+  for (int k = 0; k < 4; k++)
+    if (k < wave) before += tmp[k];
+  return before + inc - x;
+}
+
+// counts[run * BINS + digit].  in_key NULL: the first pass, keys from the tokens.
+__global__ __launch_bounds__(256) void sort_count_kernel(int N, int V, int shift, int bits, int run_keys, const int32_t* __restrict__ tokens,
+                                                         const uint32_t* __restrict__ in_key, uint32_t* __restrict__ counts) {
+  __shared__ unsigned hist[BINS];
+  hist[threadIdx.x] = 0;
+  __syncthreads();
+  const long long k0 = (long long)blockIdx.x * run_keys;
+  for (int k = threadIdx.x; k < run_keys && k0 + k < N; k += 256)
+    atomicAdd(&hist[((in_key ? in_key[k0 + k] : key_of(tokens[k0 + k], V)) >> shift) & ((1u << bits) - 1)], 1u);
+  __syncthreads();
+  counts[blockIdx.x * BINS + threadIdx.x] = hist[threadIdx.x];
+}
+
+// in_key, in_pos NULL: the first pass, positions in order.
+__global__ __launch_bounds__(256) void sort_place_kernel(int N, int V, int shift, int bits, int run_keys, int runs, const int32_t* __restrict__ tokens,
+                                                         const uint32_t* __restrict__ in_key, const uint32_t* __restrict__ in_pos,
+                                                         const uint32_t* __restrict__ counts,
+                                                         uint32_t* __restrict__ out_key, uint32_t* __restrict__ out_pos) {
+  __shared__ unsigned next[4][BINS];
+  __shared__ unsigned tmp[4];
+  const int run = blockIdx.x, wave = threadIdx.x >> 6, d = threadIdx.x;
+  const long long k0 = (long long)run * run_keys;
+  const int n = (int)min((long long)run_keys, N - k0), per_wave = run_keys / 4;
+  // keys of digit d in the runs before this one, and in all
+  unsigned before = 0, total = 0;
+#pragma unroll 8
+  for (int r = 0; r < runs; r++) {
+    const unsigned c = counts[r * BINS + d];
+    if (r < run) before += c;
+    total += c;
+  }
+#pragma unroll
+  for (int w = 0; w < 4; w++) next[w][d] = 0;
+  const unsigned start = scan256(total, tmp) + before;
+  __syncthreads();
+  for (int k = threadIdx.x & 63; k < per_wave && wave * per_wave + k < n; k += 64) {
+    const long long at = k0 + wave * per_wave + k;
+    atomicAdd(&next[wave][((in_key ? in_key[at] : key_of(tokens[at], V)) >> shift) & ((1u << bits) - 1)], 1u);
+  }
+  __syncthreads();
+  unsigned x = start;
+#pragma unroll
+  for (int w = 0; w < 4; w++) {
+    const unsigned c = next[w][d];
+    next[w][d] = x;
+    x += c;
+  }
+  __syncthreads();
+  place_keys(
+      n, per_wave, shift, bits, next[wave],
+      [&](int k, unsigned& key, unsigned& pos) {
+        key = in_key ? in_key[k0 + k] : key_of(tokens[k0 + k], V);
+        pos = in_pos ? in_pos[k0 + k] : (unsigned)(k0 + k);
+      },
+      [&](unsigned to, unsigned key, unsigned pos) {
+        out_key[to] = key;
+        out_pos[to] = pos;
+      });
+}
+
+// All passes by one workgroup, keys in LDS.
+__global__ __launch_bounds__(1024) void sort_small_kernel(int N, int V, int bits, int passes, const int32_t* __restrict__ tokens,
+                                                          uint32_t* __restrict__ out_key, uint32_t* __restrict__ out_pos) {
+  extern __shared__ unsigned lds[];
+  unsigned* next = lds;                // [16][BINS]
+  unsigned* tmp = next + 16 * BINS;    // [16]
+  unsigned* key[2] = {tmp + 16, tmp + 16 + N};
+  unsigned* pos[2] = {tmp + 16 + 2 * N, tmp + 16 + 3 * N};
+  const int wave = threadIdx.x >> 6, per_wave = ((N + 15) / 16 + 63) / 64 * 64;
+  for (int k = threadIdx.x; k < N; k += 1024) {
+    key[0][k] = key_of(tokens[k], V);
+    pos[0][k] = k;
+  }
+  for (int p = 0; p < passes; p++) {
+    const int shift = p * bits;
+    const unsigned *ik = key[p & 1], *ip = pos[p & 1];
+    for (int i = threadIdx.x; i < 16 * BINS; i += 1024) next[i] = 0;
+    __syncthreads();
+    for (int k = wave * per_wave + (threadIdx.x & 63); k < min(N, (wave + 1) * per_wave); k += 64)
+      atomicAdd(&next[wave * BINS + ((ik[k] >> shift) & ((1u << bits) - 1))], 1u);
+    __syncthreads();
+    unsigned total = 0;
+    if (threadIdx.x < BINS)
+      for (int w = 0; w < 16; w++) total += next[w * BINS + threadIdx.x];
+    unsigned x = scan256(total, tmp);
+    if (threadIdx.x < BINS)
+      for (int w = 0; w < 16; w++) {
+        const unsigned c = next[w * BINS + threadIdx.x];
+        next[w * BINS + threadIdx.x] = x;
+        x += c;
+      }
+    __syncthreads();
+    unsigned* ok = p + 1 < passes ? key[(p + 1) & 1] : out_key;
+    unsigned* op = p + 1 < passes ? pos[(p + 1) & 1] : out_pos;
+    place_keys(
+        N, per_wave, shift, bits, next + wave * BINS,
+        [&](int k, unsigned& a, unsigned& b) {
+          a = ik[k];
+          b = ip[k];
+        },
+        [&](unsigned to, unsigned a, unsigned b) {
+          ok[to] = a;
+          op[to] = b;
+        });
+    __syncthreads();
   }
 }
 
 // ---- sums -------------------------------------------------------------------------------------------
-// acc += rows pos[k0 .. k1) of dout, E features from d0.
-template <typename T, int E>
-__device__ __forceinline__ void add_rows(float (&acc)[E], const T* __restrict__ dout, int D, int d0, const uint32_t* __restrict__ pos, int k0, int k1) {
-  for (int k = k0; k < k1; k++) {
-    const T* row = dout + (size_t)pos[k] * D + d0;
-    if (E > 1) {
-      Vec16<T> x;
-      x.load(row);
+// A wavefront's piece of a row: STEPS x 64 vectors of E elements, from feature d0 on.  Loads beyond the row are loads of its end again: without
+// branches, those of several rows are in flight together.
+template <int E, int STEPS>
+struct Piece {
+  static constexpr int WIDTH = STEPS * 64 * E;
+  float x[STEPS][E];
+  int at[STEPS];  // features of this lane
+  __device__ __forceinline__ Piece(int d0) {
 #pragma unroll
-      for (int e = 0; e < E; e++) acc[e] += x.get(e);
-    } else {
-      acc[0] += to_f(row[0]);
+    for (int s = 0; s < STEPS; s++) {
+      at[s] = d0 + (s * 64 + (threadIdx.x & 63)) * E;
+#pragma unroll
+      for (int e = 0; e < E; e++) x[s][e] = 0.f;
+    }
+  }
+  // += R rows, in order
+  template <int R, typename T>
+  __device__ __forceinline__ void add(const T* const (&row)[R], int D) {
+    typedef std::conditional_t<E == 1, T, std::conditional_t<sizeof(T) == 4, float4, uint2>> Vec;
+    Vec v[R][STEPS];
+#pragma unroll
+    for (int r = 0; r < R; r++)
+#pragma unroll
+      for (int s = 0; s < STEPS; s++) v[r][s] = *reinterpret_cast<const Vec*>(row[r] + min(at[s], D - E));
+#pragma unroll
+    for (int r = 0; r < R; r++)
+#pragma unroll
+      for (int s = 0; s < STEPS; s++) {
+        if constexpr (E == 1) {
+          x[s][0] += to_f(v[r][s]);
+        } else if constexpr (sizeof(T) == 4) {
+          x[s][0] += v[r][s].x; x[s][1] += v[r][s].y; x[s][2] += v[r][s].z; x[s][3] += v[r][s].w;
+        } else {
+          x[s][0] += __uint_as_float(v[r][s].x << 16); x[s][1] += __uint_as_float(v[r][s].x & 0xffff0000u);
+          x[s][2] += __uint_as_float(v[r][s].y << 16); x[s][3] += __uint_as_float(v[r][s].y & 0xffff0000u);
+        }
+      }
+  }
+  // scale, add to what is there where asked, store
+  __device__ __forceinline__ void store(float* __restrict__ row, int D, float scale, bool accumulate) const {
+#pragma unroll
+    for (int s = 0; s < STEPS; s++) {
+      if (at[s] >= D) continue;
+      float* p = row + at[s];
+      if constexpr (E == 1) {
+        *p = accumulate ? fmaf(x[s][0], scale, *p) : x[s][0] * scale;
+      } else {
+        Vec16<float> o;
+        o.raw = accumulate ? *reinterpret_cast<const float4*>(p) : make_float4(0.f, 0.f, 0.f, 0.f);
+        o.raw.x = fmaf(x[s][0], scale, o.raw.x); o.raw.y = fmaf(x[s][1], scale, o.raw.y);
+        o.raw.z = fmaf(x[s][2], scale, o.raw.z); o.raw.w = fmaf(x[s][3], scale, o.raw.w);
+        o.store_nt(p);
+      }
+    }
+  }
+};
+
+// acc += the rows of positions pos[k0 .. k1): 64 positions loaded at a time and handed around, four rows in flight.
+template <typename T, int E, int STEPS>
+__device__ __forceinline__ void add_positions(Piece<E, STEPS>& acc, const T* __restrict__ dout, int D, const uint32_t* __restrict__ pos, int k0, int k1) {
+  const int lane = threadIdx.x & 63;
+  for (int k = k0; k < k1; k += 64) {
+    const int n = min(64, k1 - k);
+    const int mine = (int)(lane < n ? pos[k + lane] : 0u);
+    auto row = [&](int i) { return dout + (size_t)(unsigned)__builtin_amdgcn_readlane(mine, i) * D; };
+    int i = 0;
+    for (; i + 4 <= n; i += 4) {
+      const T* const r[4] = {row(i), row(i + 1), row(i + 2), row(i + 3)};
+      acc.add(r, D);
+    }
+    for (; i < n; i++) {
+      const T* const r[1] = {row(i)};
+      acc.add(r, D);
     }
   }
 }
 
-template <typename T, int E>
+__device__ __forceinline__ bool whole_chunk(const uint32_t* __restrict__ key, int N, int V, int c) {
+  const int k = c * CHUNK;
+  return c >= 0 && k + CHUNK <= N && key[k] < (unsigned)V && key[k] == key[k + CHUNK - 1];
+}
+
+template <typename T, int E, int STEPS>
 __global__ __launch_bounds__(256) void embedding_chunk_kernel(int N, int V, int D, const uint32_t* __restrict__ key, const uint32_t* __restrict__ pos,
                                                               const T* __restrict__ dout, float* __restrict__ sums) {
-  const int k0 = blockIdx.x * CHUNK;
-  if (k0 + CHUNK > N) return;
-  const unsigned id = key[k0];
-  if (id >= (unsigned)V || key[k0 + CHUNK - 1] != id) return;
-  for (int d0 = threadIdx.x * E; d0 < D; d0 += 256 * E) {
-    float acc[E];
+  const int c = blockIdx.x * 4 + (threadIdx.x >> 6);
+  if (!whole_chunk(key, N, V, c)) return;
+  for (int d0 = 0; d0 < D; d0 += Piece<E, STEPS>::WIDTH) {
+    Piece<E, STEPS> acc(d0);
+    add_positions(acc, dout, D, pos, c * CHUNK, (c + 1) * CHUNK);
 #pragma unroll
-    for (int e = 0; e < E; e++) acc[e] = 0.f;
-    add_rows<T, E>(acc, dout, D, d0, pos, k0, k0 + CHUNK);
+    for (int s = 0; s < STEPS; s++)
+      if (acc.at[s] < D)
 #pragma unroll
-    for (int e = 0; e < E; e++) sums[(size_t)blockIdx.x * D + d0 + e] = acc[e];
+        for (int e = 0; e < E; e++) sums[(size_t)c * D + acc.at[s] + e] = acc.x[s][e];
   }
 }
 
@@ -212,53 +387,151 @@ __global__ __launch_bounds__(256) void embedding_chunk_kernel(int N, int V, int 
 __device__ __forceinline__ int lower_bound(const uint32_t* __restrict__ key, int n, unsigned v) {
   int lo = 0, hi = n;  // the answer is in [lo, hi]
   const int lane = threadIdx.x & 63;
-  while (hi - lo > 0) {
+  while (hi > lo) {
     const int step = (hi - lo + 63) / 64;
     const long long at = lo + (long long)lane * step;  // candidates lo, lo + step, ...
     const bool less = at < hi && key[at] < v;
     const int c = __popcll(__builtin_amdgcn_ballot_w64(less));  // sorted: the first c are less
-    if (c == 0) return lo;
-    const int nlo = lo + (c - 1) * step + 1;
+    if (c == 0) break;
     hi = min(hi, lo + c * step);
-    lo = nlo;
+    lo += (c - 1) * step + 1;
   }
-  return lo;
+  return __builtin_amdgcn_readfirstlane(lo);
 }
 
-// BY_ROW: workgroup = row of the table, zeros where no position holds it.  Otherwise workgroup = sorted position, the first of an id adds.
-template <typename T, int E, bool BY_ROW>
-__global__ __launch_bounds__(256) void embedding_rows_kernel(int N, int V, int D, const uint32_t* __restrict__ key, const uint32_t* __restrict__ pos,
-                                                             const T* __restrict__ dout, const float* __restrict__ sums, float scale, int accumulate,
-                                                             float* __restrict__ dtable) {
-  unsigned v;
-  int lo;
+// The row of an id that has whole chunks, the first of them c: a workgroup.
+template <typename T, int E, int STEPS>
+__device__ __forceinline__ void long_row(int N, int D, int c, const uint32_t* __restrict__ key, const uint32_t* __restrict__ pos, const T* __restrict__ dout,
+                                         const float* __restrict__ sums, float scale, bool accumulate, float* __restrict__ dtable, float* lds) {
+  const unsigned v = key[c * CHUNK];
+  const int wave = __builtin_amdgcn_readfirstlane(threadIdx.x >> 6), lane = threadIdx.x & 63;
+  // the positions before the first whole chunk: fewer than CHUNK
+  const int back = c * CHUNK - 1 - lane;
+  const int lo = c * CHUNK - __popcll(__builtin_amdgcn_ballot_w64(lane < CHUNK && back >= 0 && key[max(back, 0)] == v));
+  const int hi = c * CHUNK + lower_bound(key + c * CHUNK, N - c * CHUNK, v + 1);
+  const int c1 = hi / CHUNK, per = (c1 - c + 3) / 4;
+  for (int d0 = 0; d0 < D; d0 += Piece<E, STEPS>::WIDTH) {
+    Piece<E, STEPS> acc(d0);
+    if (wave == 0) add_positions(acc, dout, D, pos, lo, c * CHUNK);
+    int k = c + wave * per;
+    const int end = min(c1, k + per);
+    auto row = [&](int i) { return sums + (size_t)i * D; };
+    for (; k + 4 <= end; k += 4) {
+      const float* const r[4] = {row(k), row(k + 1), row(k + 2), row(k + 3)};
+      acc.add(r, D);
+    }
+    for (; k < end; k++) {
+      const float* const r[1] = {row(k)};
+      acc.add(r, D);
+    }
+    if (wave == 3) add_positions(acc, dout, D, pos, c1 * CHUNK, hi);
+    __syncthreads();
+    if (wave > 0)
+#pragma unroll
+      for (int s = 0; s < STEPS; s++)
+#pragma unroll
+        for (int e = 0; e < E; e++) lds[((wave - 1) * STEPS * E + s * E + e) * 64 + lane] = acc.x[s][e];
+    __syncthreads();
+    if (wave == 0) {
+      for (int w = 0; w < 3; w++)
+#pragma unroll
+        for (int s = 0; s < STEPS; s++)
+#pragma unroll
+          for (int e = 0; e < E; e++) acc.x[s][e] += lds[(w * STEPS * E + s * E + e) * 64 + lane];
+      acc.store(dtable + (size_t)v * D, D, scale, accumulate);
+    }
+  }
+}
+
+// The first `chunk_blocks` workgroups: rows with whole chunks.  The others, a wavefront each: BY_ROW, ROWS rows of the table, with zeros where no
+// position holds them; otherwise ROWS sorted positions, of which the first of an id adds (what comes without an id's first is another's).
+template <typename T, int E, int STEPS, bool BY_ROW>
+__global__ __launch_bounds__(256) void embedding_rows_kernel(int N, int V, int D, int chunk_blocks, const uint32_t* __restrict__ key,
+                                                             const uint32_t* __restrict__ pos, const T* __restrict__ dout, const float* __restrict__ sums,
+                                                             float scale, int accumulate, float* __restrict__ dtable) {
+  __shared__ float lds[3 * STEPS * E * 64];
+  if ((int)blockIdx.x < chunk_blocks) {
+    const int c = blockIdx.x;
+    if (!whole_chunk(key, N, V, c)) return;
+    if (whole_chunk(key, N, V, c - 1) && key[c * CHUNK - 1] == key[c * CHUNK]) return;  // not the first of its id
+    long_row<T, E, STEPS>(N, D, c, key, pos, dout, sums, scale, accumulate, dtable, lds);
+    return;
+  }
+  const int item = ((int)blockIdx.x - chunk_blocks) * 4 + __builtin_amdgcn_readfirstlane(threadIdx.x >> 6);
+  const int lane = threadIdx.x & 63;
+  unsigned v, v_end;
+  int lo, stop = N;  // positions are looked for from lo on
   if (BY_ROW) {
-    v = blockIdx.x;
+    if ((long long)item * ROWS >= V) return;
+    v = item * ROWS;
+    v_end = min((unsigned)V, v + ROWS);
     lo = lower_bound(key, N, v);
   } else {
-    lo = blockIdx.x;
+    if ((long long)item * ROWS >= N) return;
+    lo = item * ROWS;
+    stop = min(N, lo + ROWS);
+    if (lo > 0)  // positions of an id that begins before: not this wavefront's
+      while (lo < stop && key[lo] == key[lo - 1]) lo++;
+    if (lo >= stop || key[lo] >= (unsigned)V) return;
     v = key[lo];
-    if (v >= (unsigned)V || (lo > 0 && key[lo - 1] == v)) return;
+    v_end = V;
   }
-  int hi = lo;
-  if (lo < N && key[lo] == v) hi = lo + lower_bound(key + lo, N - lo, v + 1);
-  const int c0 = (lo + CHUNK - 1) / CHUNK, c1 = hi / CHUNK;  // whole chunks
-  for (int d0 = threadIdx.x * E; d0 < D; d0 += 256 * E) {
-    float acc[E];
-#pragma unroll
-    for (int e = 0; e < E; e++) acc[e] = 0.f;
-    if (c0 < c1) {
-      add_rows<T, E>(acc, dout, D, d0, pos, lo, c0 * CHUNK);
-      for (int c = c0; c < c1; c++)
-#pragma unroll
-        for (int e = 0; e < E; e++) acc[e] += sums[(size_t)c * D + d0 + e];
-      add_rows<T, E>(acc, dout, D, d0, pos, c1 * CHUNK, hi);
-    } else {
-      add_rows<T, E>(acc, dout, D, d0, pos, lo, hi);
+  for (; v < v_end;) {
+    // the run [lo, hi) of id v; 64 or more in sight hold a whole chunk
+    const unsigned k = lo + lane < N ? key[lo + lane] : (unsigned)V;
+    const unsigned long long same = __builtin_amdgcn_ballot_w64(k == v);
+    int n = __popcll(same);
+    if (n == 64) n = lower_bound(key + lo, N - lo, v + 1);
+    const int hi = lo + n;
+    if ((lo + CHUNK - 1) / CHUNK >= hi / CHUNK) {
+      for (int d0 = 0; d0 < D; d0 += Piece<E, STEPS>::WIDTH) {
+        Piece<E, STEPS> acc(d0);
+        add_positions(acc, dout, D, pos, lo, hi);
+        acc.store(dtable + (size_t)v * D, D, scale, accumulate);
+      }
     }
-    float* o = dtable + (size_t)v * D + d0;
+    lo = hi;
+    if (BY_ROW) {
+      v++;
+    } else {
+      if (lo >= stop) return;
+      v = __builtin_amdgcn_readfirstlane(key[lo]);
+    }
+  }
+}
+
+// Few positions: a wavefront to a row of the table (BY_ROW) or to a position, which does its id's row if it is the first that holds it.
+template <typename T, int E, int STEPS, bool BY_ROW>
+__global__ __launch_bounds__(256) void embedding_direct_kernel(int N, int V, int D, const int32_t* __restrict__ tokens, const T* __restrict__ dout, float scale,
+                                                               int accumulate, float* __restrict__ dtable) {
+  const int item = blockIdx.x * 4 + __builtin_amdgcn_readfirstlane(threadIdx.x >> 6), lane = threadIdx.x & 63;
+  if (item >= (BY_ROW ? V : N)) return;
+  const int v = BY_ROW ? item : __builtin_amdgcn_readfirstlane(tokens[item]);
+  if (!BY_ROW && (v < 0 || v >= V)) return;
+  unsigned long long hold[DIRECT / 64];  // which positions hold it
 #pragma unroll
-    for (int e = 0; e < E; e++) o[e] = accumulate ? fmaf(acc[e], scale, o[e]) : acc[e] * scale;
+  for (int w = 0; w < DIRECT / 64; w++) {
+    const int n = w * 64 + lane;
+    hold[w] = __builtin_amdgcn_ballot_w64(n < N && tokens[min(n, N - 1)] == v);
+  }
+  if (!BY_ROW) {
+    unsigned long long before = 0;
+#pragma unroll
+    for (int w = 0; w < DIRECT / 64; w++) {
+      const int at = item - w * 64;
+      before |= at >= 64 ? hold[w] : at > 0 ? hold[w] & ((1ull << at) - 1) : 0ull;
+    }
+    if (before) return;
+  }
+  for (int d0 = 0; d0 < D; d0 += Piece<E, STEPS>::WIDTH) {
+    Piece<E, STEPS> acc(d0);
+#pragma unroll
+    for (int w = 0; w < DIRECT / 64; w++)
+      for (unsigned long long m = hold[w]; m; m &= m - 1) {
+        const T* const r[1] = {dout + (size_t)(w * 64 + __builtin_ctzll(m)) * D};
+        acc.add(r, D);
+      }
+    acc.store(dtable + (size_t)v * D, D, scale, accumulate);
   }
 }
 
@@ -267,26 +540,58 @@ struct EmbeddingWs {
 };
 static EmbeddingWs embedding_ws(int N, int V, int D) {
   const SortPlan p = sort_plan(N, V);
-  EmbeddingWs w;
+  EmbeddingWs w = {};
   size_t o = 0;
   auto take = [&](size_t bytes) { const size_t r = o; o += (bytes + 255) / 256 * 256; return r; };
-  for (int i = 0; i < 2; i++) {
-    w.key[i] = take((size_t)N * 4);
-    w.pos[i] = take((size_t)N * 4);
+  if (N > DIRECT) {
+    for (int i = 0; i < 2; i++) {
+      w.key[i] = take((size_t)N * 4);
+      w.pos[i] = take((size_t)N * 4);
+    }
+    w.counts = take((size_t)p.runs * BINS * 4);
+    w.sums = take((size_t)(N / CHUNK) * D * 4);
   }
-  w.counts = take((size_t)p.waves * ((size_t)1 << p.bits) * 4);
-  w.sums = take((size_t)(N / CHUNK) * D * 4);
-  w.total = o;
+  w.total = o ? o : 256;  // (never none: a caller's empty allocation has no address)
   return w;
 }
 size_t embedding_bwd_ws_bytes(int N, int V, int D) { return embedding_ws(N, V, D).total; }
 
-template <typename T, int E>
-static int embedding_sums(int N, int V, int D, const uint32_t* key, const uint32_t* pos, const T* dout, float* sums, float scale, float* dtable,
-                          bool accumulate, hipStream_t s) {
-  if (N >= CHUNK) hipLaunchKernelGGL((embedding_chunk_kernel<T, E>), dim3(N / CHUNK), dim3(256), 0, s, N, V, D, key, pos, dout, sums);
-  if (accumulate) hipLaunchKernelGGL((embedding_rows_kernel<T, E, false>), dim3(N), dim3(256), 0, s, N, V, D, key, pos, dout, sums, scale, 1, dtable);
-  else hipLaunchKernelGGL((embedding_rows_kernel<T, E, true>), dim3(V), dim3(256), 0, s, N, V, D, key, pos, dout, sums, scale, 0, dtable);
+template <typename T, int E, int STEPS>
+static int embedding_bwd_t(int N, int V, int D, const int32_t* tokens, const T* dout, float scale, float* dtable, bool accumulate, char* ws, hipStream_t s) {
+  if (N <= DIRECT) {
+    const dim3 grid(((accumulate ? N : V) + 3) / 4);
+    if (accumulate) hipLaunchKernelGGL((embedding_direct_kernel<T, E, STEPS, false>), grid, dim3(256), 0, s, N, V, D, tokens, dout, scale, 1, dtable);
+    else hipLaunchKernelGGL((embedding_direct_kernel<T, E, STEPS, true>), grid, dim3(256), 0, s, N, V, D, tokens, dout, scale, 0, dtable);
+    FAX_LAUNCH_CHECK("embedding_bwd");
+    return FAX_OK;
+  }
+  const SortPlan p = sort_plan(N, V);
+  const EmbeddingWs w = embedding_ws(N, V, D);
+  uint32_t *key = nullptr, *pos = nullptr;
+  if (N <= SMALL_KEYS) {
+    key = (uint32_t*)(ws + w.key[0]);
+    pos = (uint32_t*)(ws + w.pos[0]);
+    const size_t lds = (16 * BINS + 16 + 4 * (size_t)N) * 4;
+    FAX_HIP(hipFuncSetAttribute(reinterpret_cast<const void*>(sort_small_kernel), hipFuncAttributeMaxDynamicSharedMemorySize,
+                                (16 * BINS + 16 + 4 * SMALL_KEYS) * 4));
+    hipLaunchKernelGGL(sort_small_kernel, dim3(1), dim3(1024), lds, s, N, V, p.bits, p.passes, tokens, key, pos);
+  } else {
+    uint32_t* counts = (uint32_t*)(ws + w.counts);
+    for (int i = 0; i < p.passes; i++) {
+      uint32_t *ok = (uint32_t*)(ws + w.key[i & 1]), *op = (uint32_t*)(ws + w.pos[i & 1]);
+      hipLaunchKernelGGL(sort_count_kernel, dim3(p.runs), dim3(256), 0, s, N, V, i * p.bits, p.bits, p.run_keys, tokens, key, counts);
+      hipLaunchKernelGGL(sort_place_kernel, dim3(p.runs), dim3(256), 0, s, N, V, i * p.bits, p.bits, p.run_keys, p.runs, tokens, key, pos, counts, ok, op);
+      key = ok;
+      pos = op;
+    }
+  }
+  float* sums = (float*)(ws + w.sums);
+  const int chunks = N / CHUNK;
+  hipLaunchKernelGGL((embedding_chunk_kernel<T, E, STEPS>), dim3((chunks + 3) / 4), dim3(256), 0, s, N, V, D, key, pos, dout, sums);
+  const int items = ((accumulate ? N : V) + ROWS - 1) / ROWS;
+  const dim3 grid(chunks + (items + 3) / 4);
+  if (accumulate) hipLaunchKernelGGL((embedding_rows_kernel<T, E, STEPS, false>), grid, dim3(256), 0, s, N, V, D, chunks, key, pos, dout, sums, scale, 1, dtable);
+  else hipLaunchKernelGGL((embedding_rows_kernel<T, E, STEPS, true>), grid, dim3(256), 0, s, N, V, D, chunks, key, pos, dout, sums, scale, 0, dtable);
   FAX_LAUNCH_CHECK("embedding_bwd");
   return FAX_OK;
 }
@@ -295,26 +600,24 @@ int embedding_bwd(int dtype, int N, int V, int D, const int32_t* tokens, const v
                   hipStream_t s) {
   if (N == 0) return accumulate ? FAX_OK : fill_zero(dtable, (size_t)V * D * 4, s);
   Timed t_("embedding_bwd", WORK_BYTE, (double)N * D * (dtype == FAX_F32 ? 4.0 : 2.0) + (accumulate ? 8.0 * D * (N < V ? N : V) : 4.0 * V * D), s);
-  const SortPlan p = sort_plan(N, V);
-  const EmbeddingWs w = embedding_ws(N, V, D);
-  char* b = (char*)ws;
-  uint32_t* counts = (uint32_t*)(b + w.counts);
-  uint32_t *key = nullptr, *pos = nullptr;
-  const unsigned grid = (p.waves + 3) / 4;
-  for (int i = 0; i < p.passes; i++) {
-    uint32_t *ok = (uint32_t*)(b + w.key[i & 1]), *op = (uint32_t*)(b + w.pos[i & 1]);
-    hipLaunchKernelGGL(sort_count_kernel, dim3(grid), dim3(256), 0, s, N, V, i * p.bits, p.bits, p.per_wave, p.waves, tokens, key, counts);
-    hipLaunchKernelGGL(sort_scan_kernel, dim3(1), dim3(1024), 0, s, p.waves << p.bits, counts);
-    hipLaunchKernelGGL(sort_place_kernel, dim3(grid), dim3(256), 0, s, N, V, i * p.bits, p.bits, p.per_wave, p.waves, tokens, key, pos, counts, ok, op);
-    key = ok;
-    pos = op;
-  }
-  float* sums = (float*)(b + w.sums);
-  if (dtype == FAX_F32)
-    return D % 4 == 0 ? embedding_sums<float, 4>(N, V, D, key, pos, (const float*)dout, sums, scale, dtable, accumulate, s)
-                      : embedding_sums<float, 1>(N, V, D, key, pos, (const float*)dout, sums, scale, dtable, accumulate, s);
-  return D % 8 == 0 ? embedding_sums<bf16_t, 8>(N, V, D, key, pos, (const bf16_t*)dout, sums, scale, dtable, accumulate, s)
-                    : embedding_sums<bf16_t, 1>(N, V, D, key, pos, (const bf16_t*)dout, sums, scale, dtable, accumulate, s);
+  // steps of a wavefront across a row: up to four, as even as they come out
+  const int e = D % 4 == 0 ? 4 : 1, n = (D + 64 * e - 1) / (64 * e), passes = (n + 3) / 4, steps = (n + passes - 1) / passes;
+  auto by_steps = [&](auto rows, auto vec) -> int {
+    typedef std::remove_pointer_t<decltype(rows)> T;
+    constexpr int E = decltype(vec)::value;
+    char* w = (char*)ws;
+    const T* d = (const T*)dout;
+    switch (steps) {
+      case 1: return embedding_bwd_t<T, E, 1>(N, V, D, tokens, d, scale, dtable, accumulate, w, s);
+      case 2: return embedding_bwd_t<T, E, 2>(N, V, D, tokens, d, scale, dtable, accumulate, w, s);
+      case 3: return embedding_bwd_t<T, E, 3>(N, V, D, tokens, d, scale, dtable, accumulate, w, s);
+      default: return embedding_bwd_t<T, E, 4>(N, V, D, tokens, d, scale, dtable, accumulate, w, s);
+    }
+  };
+  typedef std::integral_constant<int, 4> Four;
+  typedef std::integral_constant<int, 1> One;
+  if (dtype == FAX_F32) return e == 4 ? by_steps((float*)nullptr, Four{}) : by_steps((float*)nullptr, One{});
+  return e == 4 ? by_steps((bf16_t*)nullptr, Four{}) : by_steps((bf16_t*)nullptr, One{});
 }
 
 }  // namespace fax
