@@ -190,38 +190,49 @@ __global__ __launch_bounds__(256) void sort_count_kernel(int N, int V, int shift
 }
 
 // in_key, in_pos NULL: the first pass, positions in order.
-__global__ __launch_bounds__(256) void sort_place_kernel(int N, int V, int shift, int bits, int run_keys, int runs, const int32_t* __restrict__ tokens,
-                                                         const uint32_t* __restrict__ in_key, const uint32_t* __restrict__ in_pos,
-                                                         const uint32_t* __restrict__ counts,
-                                                         uint32_t* __restrict__ out_key, uint32_t* __restrict__ out_pos) {
-  __shared__ unsigned next[4][BINS];
-  __shared__ unsigned tmp[4];
-  const int run = blockIdx.x, wave = threadIdx.x >> 6, d = threadIdx.x;
+static constexpr int PLACE_WAVES = RUN_KEYS / 64;
+__global__ __launch_bounds__(64 * PLACE_WAVES) void sort_place_kernel(int N, int V, int shift, int bits, int run_keys, int runs, const int32_t* __restrict__ tokens,
+                                                                      const uint32_t* __restrict__ in_key, const uint32_t* __restrict__ in_pos,
+                                                                      const uint32_t* __restrict__ counts, uint32_t* __restrict__ out_key,
+                                                                      uint32_t* __restrict__ out_pos) {
+  constexpr int QUARTERS = PLACE_WAVES * 64 / BINS;
+  __shared__ unsigned next[PLACE_WAVES][BINS];
+  __shared__ unsigned part[2][QUARTERS][BINS], tmp[4];
+  const int run = blockIdx.x, wave = threadIdx.x >> 6, d = threadIdx.x % BINS, quarter = threadIdx.x / BINS;
   const long long k0 = (long long)run * run_keys;
-  const int n = (int)min((long long)run_keys, N - k0), per_wave = run_keys / 4;
+  const int n = (int)min((long long)run_keys, N - k0), per_wave = run_keys / PLACE_WAVES;
+  for (int i = threadIdx.x; i < PLACE_WAVES * BINS; i += 64 * PLACE_WAVES) (&next[0][0])[i] = 0;
   // keys of digit d in the runs before this one, and in all
   unsigned before = 0, total = 0;
 #pragma unroll 8
-  for (int r = 0; r < runs; r++) {
+  for (int r = quarter; r < runs; r += QUARTERS) {
     const unsigned c = counts[r * BINS + d];
     if (r < run) before += c;
     total += c;
   }
-#pragma unroll
-  for (int w = 0; w < 4; w++) next[w][d] = 0;
-  const unsigned start = scan256(total, tmp) + before;
+  part[0][quarter][d] = before;
+  part[1][quarter][d] = total;
   __syncthreads();
   for (int k = threadIdx.x & 63; k < per_wave && wave * per_wave + k < n; k += 64) {
     const long long at = k0 + wave * per_wave + k;
     atomicAdd(&next[wave][((in_key ? in_key[at] : key_of(tokens[at], V)) >> shift) & ((1u << bits) - 1)], 1u);
   }
-  __syncthreads();
-  unsigned x = start;
+  before = total = 0;
 #pragma unroll
-  for (int w = 0; w < 4; w++) {
-    const unsigned c = next[w][d];
-    next[w][d] = x;
-    x += c;
+  for (int q = 0; q < QUARTERS; q++) {
+    before += part[0][q][d];
+    total += part[1][q][d];
+  }
+  const unsigned start = scan256(total, tmp) + before;  // (of the first 256 threads; what the others have is not used)
+  __syncthreads();
+  if (threadIdx.x < BINS) {
+    unsigned x = start;
+#pragma unroll
+    for (int w = 0; w < PLACE_WAVES; w++) {
+      const unsigned c = next[w][d];
+      next[w][d] = x;
+      x += c;
+    }
   }
   __syncthreads();
   place_keys(
@@ -580,7 +591,7 @@ static int embedding_bwd_t(int N, int V, int D, const int32_t* tokens, const T* 
     for (int i = 0; i < p.passes; i++) {
       uint32_t *ok = (uint32_t*)(ws + w.key[i & 1]), *op = (uint32_t*)(ws + w.pos[i & 1]);
       hipLaunchKernelGGL(sort_count_kernel, dim3(p.runs), dim3(256), 0, s, N, V, i * p.bits, p.bits, p.run_keys, tokens, key, counts);
-      hipLaunchKernelGGL(sort_place_kernel, dim3(p.runs), dim3(256), 0, s, N, V, i * p.bits, p.bits, p.run_keys, p.runs, tokens, key, pos, counts, ok, op);
+      hipLaunchKernelGGL(sort_place_kernel, dim3(p.runs), dim3(64 * PLACE_WAVES), 0, s, N, V, i * p.bits, p.bits, p.run_keys, p.runs, tokens, key, pos, counts, ok, op);
       key = ok;
       pos = op;
     }
