@@ -2,7 +2,7 @@
 // alignment, and the choice between them and the matrix-core kernels.
 #include <initializer_list>
 
-#include "attn_window.h"
+#include "window_tiles.h"
 
 namespace fax {
 
@@ -48,37 +48,111 @@ static WindowArgs window_args(const FaxWindowDims& d) {
   return a;
 }
 
+// Joins the parts that the workgroups of a cut row left, their sums undivided, with their reference points and denominators: one wavefront to a
+// row.  octaves: of the reference points' unit; unit: of it in scaled scores.  What one wavefront loads at once are all parts' points and up to eight
+// parts' sums.
+template <typename T>
+__global__ __launch_bounds__(256) void window_join_kernel(WindowArgs a, int splits, const float* __restrict__ part_o, const float2* __restrict__ part_ml,
+                                                          float octaves, float unit) {
+  const long long row = (long long)blockIdx.x * 4 + (threadIdx.x >> 6), rows = (long long)a.B * a.Hkv * a.Sq * a.group;
+  if (row >= rows) return;
+  const int lane = threadIdx.x & 63;
+  const long long per_head = (long long)a.Sq * a.group;
+  const int bh = (int)(row / per_head), r = (int)(row % per_head);
+  const int b = bh / a.Hkv, i = r / a.group, h = bh % a.Hkv * a.group + r % a.group;
+  const float2* ml = part_ml + row * splits;
+  const float* o = part_o + row * splits * a.dh;
+  // part s's point and denominator in lane s
+  const float2 mine = lane < splits ? ml[lane] : make_float2(-3.4028235e38f, 0.f);
+  const float M = wave_max(mine.x), weight = __builtin_amdgcn_exp2f((mine.x - M) * octaves);
+  const float L = wave_sum(mine.y * weight);
+  float acc[2] = {0.f, 0.f};
+  const int d0 = min(lane, a.dh - 1), d1 = min(lane + 64, a.dh - 1);
+#pragma unroll 8
+  for (int s = 0; s < splits; s++) {
+    const float w = __uint_as_float(__builtin_amdgcn_readlane(__float_as_uint(weight), s));
+    acc[0] = fmaf(o[(long long)s * a.dh + d0], w, acc[0]);
+    acc[1] = fmaf(o[(long long)s * a.dh + d1], w, acc[1]);
+  }
+  if (__any(!(fabsf(acc[0]) <= 3.4028235e38f) || !(fabsf(acc[1]) <= 3.4028235e38f)) || !(L <= 3.4028235e38f)) {
+    window_fwd_row<2, T>(a, b, i, h, lane);
+    return;
+  }
+  const bool none = L == 0.f;
+  const float inv = none ? 0.f : 1.f / L;
+  T* out = strided_row((T*)a.ctx, a.sc, b, i, h);
+#pragma unroll
+  for (int k = 0; k < 2; k++) {
+    const int d = lane + 64 * k;
+    if (d < a.dh) out[d] = from_f<T>(acc[k] * inv);
+  }
+  if (lane == 0 && a.lse) a.lse[((long long)b * a.H + h) * a.Sq + i] = none ? -INFINITY : M * unit + logf(L);
+}
+
+// The parts of the sink tiles' keys, added in order: one wavefront to a key.
+template <typename T>
+__global__ __launch_bounds__(256) void window_fold_kernel(WindowArgs a, KeyGrid kg, int tile_keys, const float* __restrict__ parts) {
+  const int keys = kg.sink_tiles * tile_keys, n = min(keys, a.Sk);
+  const int item = blockIdx.x * 4 + (threadIdx.x >> 6), lane = threadIdx.x & 63;
+  if (item >= n * a.B * a.Hkv) return;
+  const int j = item % n, bh = item / n;
+  float s[4] = {0.f, 0.f, 0.f, 0.f};  // dK and dV, two 64-wide pieces each
+  for (int p = 0; p < kg.splits; p++) {
+    const float* o = part_row(a, kg, const_cast<float*>(parts), p, bh, keys, j);
+#pragma unroll
+    for (int k = 0; k < 4; k++) {
+      const int d = lane + 64 * (k & 1);
+      if (d < a.dh) s[k] += o[(k >> 1) * a.dh + d];
+    }
+  }
+  const int b = bh / a.Hkv, hk = bh % a.Hkv;
+  if (__any((s[0] * 0.f + s[1] * 0.f) + (s[2] * 0.f + s[3] * 0.f) != 0.f)) {
+    window_dkv_row<2, T>(a, b, j, hk, lane);
+    return;
+  }
+  T* ko = strided_row((T*)a.dk, a.skv, b, j, hk);
+  T* vo = strided_row((T*)a.dv, a.skv, b, j, hk);
+#pragma unroll
+  for (int k = 0; k < 2; k++) {
+    const int d = lane + 64 * k;
+    if (d < a.dh) {
+      ko[d] = from_f<T>(s[k] * a.scale);
+      vo[d] = from_f<T>(s[2 + k]);
+    }
+  }
+}
+
 // Rows on 16 bytes, whole 16-byte chunks to a head, offsets within a tile of 64 rows in 32 bits.
-static bool strides_fit(const FaxStrides& s) { return s.batch % 8 == 0 && s.row % 8 == 0 && s.head % 8 == 0 && s.row <= (1 << 24); }
+static bool strides_fit(const FaxStrides& s, int unit) { return s.batch % unit == 0 && s.row % unit == 0 && s.head % unit == 0 && s.row <= (1 << 24); }
 
 static WindowPlan window_plan(const FaxWindowDims& d) {
   WindowPlan p = {};
   p.form = FAX_ATTENTION_SCALAR;
   p.fwd_waves = p.dq_waves = p.kv_waves = 4;
   p.fwd_splits = p.sink_splits = 1;
-  const bool fits = strides_fit(d.q) && strides_fit(d.kv) && strides_fit(d.ctx);
+  const int unit = d.dtype == FAX_F32 ? 4 : 8;
   const long long heads = (long long)d.B * d.Hkv, rows = (long long)d.Sq * (d.H / d.Hkv);
-  if (d.dtype == FAX_BF16 && d.dh % 8 == 0 && d.dh <= 128 && fits && rows < (1 << 30)) {
-    p.form = d.dh == 64 || d.dh == 128 ? FAX_ATTENTION_MFMA : FAX_ATTENTION_EDGE;
+  if (d.dh % unit == 0 && d.dh <= 128 && strides_fit(d.q, unit) && strides_fit(d.kv, unit) && strides_fit(d.ctx, unit) && rows < (1 << 30)) {
+    const bool f32 = d.dtype == FAX_F32;
+    p.form = f32 ? FAX_ATTENTION_F32 : d.dh == 64 || d.dh == 128 ? FAX_ATTENTION_MFMA : FAX_ATTENTION_EDGE;
     const long long t128 = (rows + 127) / 128 * heads, t32 = (rows + 31) / 32 * heads;
     const bool few = t128 < 256;
-    p.fwd_waves = p.dq_waves = few ? 1 : 4;
-    // tiles of keys that a row meets
+    if (!f32) p.fwd_waves = p.dq_waves = few ? 1 : 4;
+    // tiles of keys that a row meets: a run of them is at least two
     const long long seen = (long long)d.window + d.sinks + 128 < d.Sk ? d.window + d.sinks + 128 : d.Sk;
     const long long key_tiles = (seen + 63) / 64;
-    if (few && t32 < 512) {
+    if ((few || f32) && t32 < 512) {
       long long splits = 512 / t32;
       if (splits > key_tiles / 2) splits = key_tiles / 2;
-      if (splits > 64) splits = 64;
+      if (splits > 64) splits = 64;  // (a lane of the joining wavefront each)
       p.fwd_splits = splits > 1 ? (int)splits : 1;
     }
-    p.kv_waves = (d.Sk + window_dkv_keys(d.dh, 4) - 1) / window_dkv_keys(d.dh, 4) * heads < 256 ? 1 : 4;
-    const int keys = window_dkv_keys(d.dh, p.kv_waves), n = (d.Sk + keys - 1) / keys;
-    const int sinks = d.sinks < d.Sk ? d.sinks : d.Sk;
-    p.sink_tiles = (sinks + keys - 1) / keys;
-    const long long usual = (long long)d.window + keys + 64;
-    if (2 * p.sink_tiles <= n && d.Sq > usual) p.sink_splits = (int)(d.Sq / usual + 1 < 32 ? d.Sq / usual + 1 : 32);
-    if (p.sink_tiles == 0) p.sink_splits = 1;
+    if (!f32 && (d.Sk + window_dkv_keys(d.dh, 4) - 1) / window_dkv_keys(d.dh, 4) * heads < 256) p.kv_waves = 1;
+    p.kv_keys = f32 ? 32 : window_dkv_keys(d.dh, p.kv_waves);
+    const int n = (d.Sk + p.kv_keys - 1) / p.kv_keys, sinks = d.sinks < d.Sk ? d.sinks : d.Sk;
+    p.sink_tiles = (sinks + p.kv_keys - 1) / p.kv_keys;
+    const long long usual = (long long)d.window + p.kv_keys + 64;
+    if (p.sink_tiles > 0 && 2 * p.sink_tiles <= n && d.Sq > usual) p.sink_splits = (int)(d.Sq / usual + 1 < 32 ? d.Sq / usual + 1 : 32);
     if (p.sink_splits == 1) p.sink_tiles = 0;
   }
   size_t o = 0;
@@ -92,7 +166,7 @@ static WindowPlan window_plan(const FaxWindowDims& d) {
   const size_t fwd = o;
   o = 0;
   p.delta = take(all_rows * 4);
-  if (p.sink_splits > 1) p.parts = take((size_t)p.sink_splits * heads * p.sink_tiles * window_dkv_keys(d.dh, p.kv_waves) * 2 * d.dh * 4);
+  if (p.sink_splits > 1) p.parts = take((size_t)p.sink_splits * heads * p.sink_tiles * p.kv_keys * 2 * d.dh * 4);
   p.total = o > fwd ? o : fwd;
   return p;
 }
@@ -132,8 +206,20 @@ int window_fwd(const FaxWindowDims& d, const void* q, const void* k, const void*
   a.q = q; a.k = k; a.v = v; a.q_pos = q_pos; a.k_len = k_len; a.ctx = ctx; a.lse = lse;
   const WindowPlan p = window_plan(d);
   char* w = (char*)ws;
-  if (p.form != FAX_ATTENTION_SCALAR && on16({q, k, v, ctx})) FAX_TRY(window_fwd_mfma(a, p.fwd_waves, p.fwd_splits, (float*)(w + p.part_o), w + p.part_ml, s));
-  else FAX_TRY(rows_launch<0>(a, d.dtype, s));
+  if (p.form == FAX_ATTENTION_SCALAR || !on16({q, k, v, ctx})) {
+    FAX_TRY(rows_launch<0>(a, d.dtype, s));
+  } else {
+    float* part_o = (float*)(w + p.part_o);
+    float2* part_ml = (float2*)(w + p.part_ml);
+    if (p.form == FAX_ATTENTION_F32) FAX_TRY(window_fwd_f32(a, p.fwd_splits, part_o, part_ml, s));
+    else FAX_TRY(window_fwd_mfma(a, p.fwd_waves, p.fwd_splits, part_o, part_ml, s));
+    if (p.fwd_splits > 1) {
+      const float log2e = 1.4426950408889634f;
+      const dim3 grid((unsigned)(((long long)a.B * a.H * a.Sq + 3) / 4));
+      if (d.dtype == FAX_F32) hipLaunchKernelGGL(window_join_kernel<float>, grid, dim3(256), 0, s, a, p.fwd_splits, part_o, part_ml, log2e, 1.f);
+      else hipLaunchKernelGGL(window_join_kernel<bf16_t>, grid, dim3(256), 0, s, a, p.fwd_splits, part_o, part_ml, a.scale * log2e, a.scale);
+    }
+  }
   FAX_LAUNCH_CHECK("window_attention_fwd");
   return FAX_OK;
 }
@@ -146,14 +232,27 @@ int window_bwd(const FaxWindowDims& d, const void* q, const void* k, const void*
   const WindowPlan p = window_plan(d);
   char* w = (char*)ws;
   a.dctx = dctx; a.dq = dq; a.dk = dk; a.dv = dv; a.delta = (float*)(w + p.delta);
-  if (p.form != FAX_ATTENTION_SCALAR && on16({q, k, v, ctx, dctx, dq, dk, dv})) {
-    // dQ first: it also leaves delta, which dK and dV need
-    FAX_TRY(window_dq_mfma(a, p.dq_waves, s));
-    FAX_TRY(window_dkv_mfma(a, p.kv_waves, p.sink_tiles, p.sink_splits, (float*)(w + p.parts), s));
-  } else {
+  if (p.form == FAX_ATTENTION_SCALAR || !on16({q, k, v, ctx, dctx, dq, dk, dv})) {
     FAX_TRY(rows_launch<3>(a, d.dtype, s));
     FAX_TRY(rows_launch<1>(a, d.dtype, s));
     FAX_TRY(rows_launch<2>(a, d.dtype, s));
+  } else {
+    float* parts = (float*)(w + p.parts);
+    if (p.form == FAX_ATTENTION_F32) {
+      FAX_TRY(rows_launch<3>(a, d.dtype, s));
+      FAX_TRY(window_bwd_f32(a, p.sink_tiles, p.sink_splits, parts, s));
+    } else {
+      // dQ first: it also leaves delta, which dK and dV need
+      FAX_TRY(window_dq_mfma(a, p.dq_waves, s));
+      FAX_TRY(window_dkv_mfma(a, p.kv_waves, p.sink_tiles, p.sink_splits, parts, s));
+    }
+    if (p.sink_splits > 1) {
+      const KeyGrid kg(a, p.kv_keys, p.sink_tiles, p.sink_splits);
+      const long long keys = (long long)(p.sink_tiles * p.kv_keys < a.Sk ? p.sink_tiles * p.kv_keys : a.Sk) * a.B * a.Hkv;
+      const dim3 grid((unsigned)((keys + 3) / 4));
+      if (d.dtype == FAX_F32) hipLaunchKernelGGL(window_fold_kernel<float>, grid, dim3(256), 0, s, a, kg, p.kv_keys, parts);
+      else hipLaunchKernelGGL(window_fold_kernel<bf16_t>, grid, dim3(256), 0, s, a, kg, p.kv_keys, parts);
+    }
   }
   FAX_LAUNCH_CHECK("window_attention_bwd");
   return FAX_OK;

@@ -51,11 +51,6 @@ struct QueryStream {
   }
 };
 
-// Where a key's sums go: dK and dV, or a part's row of scratch ([part, head, key of the sink tiles, dK | dV, feature]).
-__device__ __forceinline__ float* part_row(const WindowArgs& a, const KeyGrid& k, float* parts, int split, int bh, int keys, int j) {
-  return parts + ((((long long)split * a.B * a.Hkv + bh) * keys + j) * 2) * a.dh;
-}
-
 // ---------------------------------------------------------------------------------------------
 // 32 keys to a wave.  Per 32-query half: S = Q K^T and dP = dO V^T, P and dS, dV^T += dO^T P and dK^T += Q^T dS.
 // ---------------------------------------------------------------------------------------------
@@ -409,48 +404,12 @@ __global__ __launch_bounds__(64 * WPG, 2) void window_dkv16_mfma_kernel(WindowAr
   }
 }
 
-// The parts of the sink tiles' keys, added in order: one wavefront to a key.
-__global__ __launch_bounds__(256) void window_fold_kernel(WindowArgs a, KeyGrid kg, int tile_keys, const float* __restrict__ parts) {
-  const int keys = kg.sink_tiles * tile_keys, n = min(keys, a.Sk);
-  const int item = blockIdx.x * 4 + (threadIdx.x >> 6), lane = threadIdx.x & 63;
-  if (item >= n * a.B * a.Hkv) return;
-  const int j = item % n, bh = item / n;
-  float s[4] = {0.f, 0.f, 0.f, 0.f};  // dK and dV, two 64-wide pieces each
-  for (int p = 0; p < kg.splits; p++) {
-    const float* o = part_row(a, kg, const_cast<float*>(parts), p, bh, keys, j);
-#pragma unroll
-    for (int k = 0; k < 4; k++) {
-      const int d = lane + 64 * (k & 1);
-      if (d < a.dh) s[k] += o[(k >> 1) * a.dh + d];
-    }
-  }
-  const int b = bh / a.Hkv, hk = bh % a.Hkv;
-  if (__any((s[0] * 0.f + s[1] * 0.f) + (s[2] * 0.f + s[3] * 0.f) != 0.f)) {
-    window_dkv_row<2, bf16_t>(a, b, j, hk, lane);
-    return;
-  }
-  bf16_t* ko = strided_row((bf16_t*)a.dk, a.skv, b, j, hk);
-  bf16_t* vo = strided_row((bf16_t*)a.dv, a.skv, b, j, hk);
-#pragma unroll
-  for (int k = 0; k < 2; k++) {
-    const int d = lane + 64 * k;
-    if (d < a.dh) {
-      ko[d] = (bf16_t)(s[k] * a.scale);
-      vo[d] = (bf16_t)s[2 + k];
-    }
-  }
-}
-
 int window_dkv_keys(int dh, int waves) { return (dh <= 64 ? 32 : 16) * waves; }
 
 int window_dkv_mfma(const WindowArgs& a, int waves, int sink_tiles, int splits, float* parts, hipStream_t s) {
   const int keys = window_dkv_keys(a.dh, waves), heads = a.B * a.Hkv;
-  KeyGrid kg;
-  kg.n_tiles = (a.Sk + keys - 1) / keys;
-  kg.sink_tiles = splits > 1 ? sink_tiles : 0;
-  kg.splits = splits;
-  kg.sink_blocks = (int)xcd_grid((long long)kg.sink_tiles * heads * splits);
-  const unsigned grid = kg.sink_blocks + xcd_grid((long long)(kg.n_tiles - kg.sink_tiles) * heads);
+  const KeyGrid kg(a, keys, sink_tiles, splits);
+  const unsigned grid = kg.blocks(heads);
   auto launch = [&](auto kern, size_t row) -> int {
     const size_t lds = 2 * (2 * (size_t)TR * row * 2 + 4 * 256);
     FAX_HIP(hipFuncSetAttribute(reinterpret_cast<const void*>(kern), hipFuncAttributeMaxDynamicSharedMemorySize, (int)lds));
@@ -465,12 +424,7 @@ int window_dkv_mfma(const WindowArgs& a, int waves, int sink_tiles, int splits, 
     if (a.dh <= 96) return launch(window_dkv16_mfma_kernel<96, true, W>, 128);
     return launch(window_dkv16_mfma_kernel<128, true, W>, 128);
   };
-  FAX_TRY(waves == 1 ? go(I<1>{}) : go(I<4>{}));
-  if (kg.sink_tiles) {
-    const int n = kg.sink_tiles * keys < a.Sk ? kg.sink_tiles * keys : a.Sk;
-    hipLaunchKernelGGL(window_fold_kernel, dim3((unsigned)(((long long)n * heads + 3) / 4)), dim3(256), 0, s, a, kg, keys, parts);
-  }
-  return FAX_OK;
+  return waves == 1 ? go(I<1>{}) : go(I<4>{});
 }
 
 }  // namespace fax

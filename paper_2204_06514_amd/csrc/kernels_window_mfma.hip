@@ -34,7 +34,7 @@ __global__ __launch_bounds__(64 * WPG, 2) void window_fwd_mfma_kernel(WindowArgs
   const unsigned sm = lds_addr(smem);
   if (EDGE) clear_lds(smem, 4 * TB);
 
-  const KeyTiles kt(KeyRanges(a, sq, rt.p0, rt.p1));
+  const KeyTiles<TR> kt(KeyRanges(a, sq, rt.p0, rt.p1));
   const int u0 = PART ? (int)((long long)kt.n * split / splits) : 0, u1 = PART ? (int)((long long)kt.n * (split + 1) / splits) : kt.n;
 
   bf16x8 qf[KS];
@@ -96,7 +96,7 @@ __global__ __launch_bounds__(64 * WPG, 2) void window_fwd_mfma_kernel(WindowArgs
 #pragma unroll
         for (int v = 0; v < 16; v++) {
           const int key = j0 + jt * 32 + (v >> 2) * 8 + g * 4 + (v & 3);
-          s[jt][v] = (key > last) | ((key <= first) & (key >= a.sinks)) ? -INFINITY : s[jt][v];
+          s[jt][v] = ((key > last) | ((key <= first) & (key >= a.sinks))) ? -INFINITY : s[jt][v];
         }
     }
     float mx = -INFINITY;
@@ -230,7 +230,7 @@ __global__ __launch_bounds__(64 * WPG, 2) void window_dq_mfma_kernel(WindowArgs 
   const float scale = a.scale, c = scale * LOG2E;
   const unsigned sm = lds_addr(smem);
   if (EDGE) clear_lds(smem, 4 * TB);
-  const KeyTiles kt(KeyRanges(a, sq, rt.p0, rt.p1));
+  const KeyTiles<TR> kt(KeyRanges(a, sq, rt.p0, rt.p1));
 
   bf16x8 qf[KS], dof[KS];
   const bf16_t* qp = strided_row((const bf16_t*)a.q, a.sq, b, rt.i, rt.h);
@@ -305,7 +305,7 @@ __global__ __launch_bounds__(64 * WPG, 2) void window_dq_mfma_kernel(WindowArgs 
         const float e = __builtin_amdgcn_exp2f(fmaf(sc[v], c, -li));
         float d = e * (dp[v] - di);
         const int key = j0 + jt * 32 + (v >> 2) * 8 + g * 4 + (v & 3);
-        if (MASK) d = (key > last) | ((key <= first) & (key >= a.sinks)) ? 0.f : d;
+        if (MASK) d = ((key > last) | ((key <= first) & (key >= a.sinks))) ? 0.f : d;
         ds_sum += d;
         dp[v] = d;
         if (v & 1) split2(dp[v - 1], d, db[v >> 3], dl[v >> 3], (v & 7) >> 1);
@@ -365,44 +365,6 @@ __global__ __launch_bounds__(64 * WPG, 2) void window_dq_mfma_kernel(WindowArgs 
   }
 }
 
-// Joins the parts of a row that PART workgroups left: one wavefront to a row.
-__global__ __launch_bounds__(256) void window_join_kernel(WindowArgs a, int splits, const float* __restrict__ part_o, const float2* __restrict__ part_ml,
-                                                          float octaves, float unit) {
-  const long long row = (long long)blockIdx.x * 4 + (threadIdx.x >> 6), rows = (long long)a.B * a.Hkv * a.Sq * a.group;
-  if (row >= rows) return;
-  const int lane = threadIdx.x & 63;
-  const long long per_head = (long long)a.Sq * a.group;
-  const int bh = (int)(row / per_head), r = (int)(row % per_head);
-  const int b = bh / a.Hkv, i = r / a.group, h = bh % a.Hkv * a.group + r % a.group;
-  const float2* ml = part_ml + row * splits;
-  const float* o = part_o + row * splits * a.dh;
-  float M = -3.4028235e38f;
-  for (int s = 0; s < splits; s++) M = fmaxf(M, ml[s].x);
-  float L = 0.f, acc[2] = {0.f, 0.f};
-  for (int s = 0; s < splits; s++) {
-    const float w = __builtin_amdgcn_exp2f((ml[s].x - M) * octaves);
-    L = fmaf(ml[s].y, w, L);
-#pragma unroll
-    for (int k = 0; k < 2; k++) {
-      const int d = lane + 64 * k;
-      if (d < a.dh) acc[k] = fmaf(o[(long long)s * a.dh + d], w, acc[k]);
-    }
-  }
-  if (__any(!(fabsf(acc[0]) <= 3.4028235e38f) || !(fabsf(acc[1]) <= 3.4028235e38f)) || !(L <= 3.4028235e38f)) {
-    window_fwd_row<2, bf16_t>(a, b, i, h, lane);
-    return;
-  }
-  const bool none = L == 0.f;
-  const float inv = none ? 0.f : 1.f / L;
-  bf16_t* out = strided_row((bf16_t*)a.ctx, a.sc, b, i, h);
-#pragma unroll
-  for (int k = 0; k < 2; k++) {
-    const int d = lane + 64 * k;
-    if (d < a.dh) out[d] = (bf16_t)(acc[k] * inv);
-  }
-  if (lane == 0 && a.lse) a.lse[((long long)b * a.H + h) * a.Sq + i] = none ? -INFINITY : M * unit + logf(L);
-}
-
 template <typename K>
 static int set_lds(K kern, size_t bytes) {
   FAX_HIP(hipFuncSetAttribute(reinterpret_cast<const void*>(kern), hipFuncAttributeMaxDynamicSharedMemorySize, (int)bytes));
@@ -430,13 +392,7 @@ int window_fwd_mfma(const WindowArgs& a, int waves, int splits, float* part_o, v
       hipLaunchKernelGGL(kern, dim3(xcd_grid(items)), dim3(64 * waves), lds, s, a, n_tiles, (int)items, splits, part_o, (float2*)part_ml);
       return FAX_OK;
     };
-    if (splits > 1) {
-      FAX_TRY(waves == 1 ? go(I<1>{}, T_{}) : go(I<4>{}, T_{}));
-      const long long rows = (long long)a.B * a.H * a.Sq;
-      hipLaunchKernelGGL(window_join_kernel, dim3((unsigned)((rows + 3) / 4)), dim3(256), 0, s, a, splits, part_o, (const float2*)part_ml,
-                         a.scale * LOG2E, a.scale);
-      return FAX_OK;
-    }
+    if (splits > 1) return waves == 1 ? go(I<1>{}, T_{}) : go(I<4>{}, T_{});
     return waves == 1 ? go(I<1>{}, F_{}) : go(I<4>{}, F_{});
   });
 }

@@ -8,35 +8,9 @@
 //   * Rows of a tile from the last key on are loads of the last key (never a read out of bounds, nothing left in LDS that was not loaded).
 #pragma once
 #include "attn_dkv16.h"
-#include "attn_window.h"
+#include "window_tiles.h"
 
 namespace fax {
-
-// Workgroup -> item, with neighbouring items on one XCD (workgroups go to the eight XCDs in turn): they share K and V tiles, or Q and dO, in
-// its L2.  The grid is xcd_grid(items); items that are none are out of range.
-inline unsigned xcd_grid(long long items) { return (unsigned)((items + 7) / 8 * 8); }
-__device__ __forceinline__ int xcd_item(int block, int grid) { return (block & 7) * (grid >> 3) + (block >> 3); }
-
-// 64-key tiles of a run of queries, in order: those of the sinks, then those of the window.
-struct KeyTiles {
-  int sink_tiles, skip, n;
-  __device__ __forceinline__ KeyTiles(const KeyRanges& k) {
-    sink_tiles = (k.sink_end + TR - 1) / TR;
-    const int first = max(sink_tiles, k.lo / TR);
-    skip = first - sink_tiles;
-    n = sink_tiles + (k.lo < k.end ? max(0, (k.end + TR - 1) / TR - first) : 0);
-  }
-  __device__ __forceinline__ int key(int u) const { return (u < sink_tiles ? u : u + skip) * TR; }
-};
-
-// Whether queries at p0 .. p1 see all of, or anything of, the keys j0 .. j0 + width - 1.
-__device__ __forceinline__ bool sees_all(const WindowArgs& a, int k_len, int p0, int p1, int j0, int width) {
-  const int last = j0 + width - 1;
-  return last < k_len && last <= p0 && (j0 > p1 - a.window || last < a.sinks);
-}
-__device__ __forceinline__ bool sees_any(const WindowArgs& a, int k_len, int p0, int p1, int j0, int width) {
-  return j0 < k_len && j0 <= p1 && (j0 + width - 1 > p0 - a.window || j0 < a.sinks);
-}
 
 // The same address for the whole wave, in scalar registers, whatever the compiler keeps it in.
 __device__ __forceinline__ const bf16_t* uniform(const bf16_t* p) {
@@ -117,33 +91,6 @@ struct RowTile {
     p1 = s.pos0 + min(r0 + 32 * WPG - 1, rows - 1) / a.group;
     wp0 = s.pos0 + min(w0, rows - 1) / a.group;
     wp1 = w0 < rows ? s.pos0 + min(w0 + 31, rows - 1) / a.group : -2147483647 - 1;  // (a wave without rows sees nothing)
-  }
-};
-
-// dK and dV.  A workgroup has a tile of keys of one key head and streams the 64-query tiles of all its query heads that see some of
-// them, head by head.  Keys among the sinks are seen by every later query, not by a window's length of them: their tiles' streams are cut into
-// `splits` parts, workgroups of their own that leave sums for window_fold_kernel.  They are the first workgroups of the launch; the other
-// tiles follow.
-struct KeyGrid {
-  int n_tiles, sink_tiles, splits, sink_blocks;  // key tiles of a head; how many of them are split, into how many parts; workgroups of those
-};
-struct KeyItem {
-  int bh, tile, split;  // split < 0: whole
-  bool ok;
-  __device__ __forceinline__ KeyItem(const KeyGrid& k, int heads, int block, int grid) {
-    if (block < k.sink_blocks) {
-      split = block % k.splits;
-      const int r = block / k.splits;
-      tile = r % max(k.sink_tiles, 1);
-      bh = r / max(k.sink_tiles, 1);
-      ok = bh < heads;
-    } else {
-      const int rest = k.n_tiles - k.sink_tiles, i = xcd_item(block - k.sink_blocks, grid - k.sink_blocks);
-      split = -1;
-      ok = i < rest * heads;
-      tile = k.sink_tiles + i % max(rest, 1);
-      bh = i / max(rest, 1);
-    }
   }
 };
 
