@@ -471,12 +471,14 @@ typedef struct FaxWindowDims {
 } FaxWindowDims;
 /* Host-only: what the two calls make of a size whose tensors start on 16 bytes.
  *   form         FAX_ATTENTION_*, as in FaxAttentionRoute.
- *   fwd_waves, dq_waves, kv_waves   wavefronts of a workgroup (32 rows each; 32 keys, 16 above head width 64): 4, or 1 where workgroups are few.
- *   fwd_splits   runs of keys that a row's forward pass is cut into, which a second kernel joins (1: none).
- *   sink_splits  runs of queries that the sinks' dK and dV are cut into (1: none).
+ *   waves        bf16: wavefronts of a workgroup of the forward pass and dQ, 32 rows (queries of all heads of a key head) each: 4, or 1 for
+ *                up to 32 rows.  fp32: 1, a tile of 32 rows.
+ *   row_splits   runs of keys that a row's forward pass and its dQ are cut into, which a second kernel joins (1: none).
+ *   kv_splits, cut_keys   runs of queries that dK and dV of the first cut_keys keys are cut into (1, 0: none): the sinks', which every later query
+ *                sees, or all.
  * Exposed so that a test can assert that its sizes run the form they are about. */
 typedef struct FaxWindowRoute {
-  int32_t form, fwd_waves, fwd_splits, dq_waves, kv_waves, sink_splits;
+  int32_t form, waves, row_splits, kv_splits, cut_keys;
 } FaxWindowRoute;
 int fax_window_attention_route(const FaxWindowDims* dims, FaxWindowRoute* out);
 int fax_window_attention_workspace_bytes(const FaxWindowDims* dims, size_t* out);

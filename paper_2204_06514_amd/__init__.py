@@ -92,7 +92,7 @@ class FaxWindowDims(C.Structure):
 
 
 class FaxWindowRoute(C.Structure):
-    _fields_ = [(n, C.c_int32) for n in ("form", "fwd_waves", "fwd_splits", "dq_waves", "kv_waves", "sink_splits")]
+    _fields_ = [(n, C.c_int32) for n in ("form", "waves", "row_splits", "kv_splits", "cut_keys")]
 
 
 class FaxAdamWTensor(C.Structure):

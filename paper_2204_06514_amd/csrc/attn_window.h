@@ -26,15 +26,15 @@ struct WindowArgs {
 // How a size is run (kernels_window.hip), and where its parts lie in the workspace.
 struct WindowPlan {
   int form;                                    // FAX_ATTENTION_*
-  int fwd_waves, fwd_splits, dq_waves, kv_waves, kv_keys, sink_tiles, sink_splits;  // kv_keys: keys of a workgroup
-  size_t delta, part_o, part_ml, parts, total;
+  int waves, row_splits, kv_keys, cut_tiles, kv_splits;  // kv_keys: keys of a workgroup
+  size_t delta, part_o, part_ml, part_dq, part_ds, parts, total;
 };
 int window_fwd_mfma(const WindowArgs& a, int waves, int splits, float* part_o, void* part_ml, hipStream_t s);
-int window_dq_mfma(const WindowArgs& a, int waves, hipStream_t s);
-int window_dkv_keys(int dh, int waves);  // keys of a workgroup
-int window_dkv_mfma(const WindowArgs& a, int waves, int sink_tiles, int splits, float* parts, hipStream_t s);
+int window_dq_mfma(const WindowArgs& a, int waves, int splits, float* part_dq, float* part_ds, hipStream_t s);
+int window_dkv_keys(int dh);  // keys of a workgroup
+int window_dkv_mfma(const WindowArgs& a, int cut_tiles, int splits, float* parts, hipStream_t s);
 int window_fwd_f32(const WindowArgs& a, int splits, float* part_o, void* part_ml, hipStream_t s);
-int window_bwd_f32(const WindowArgs& a, int sink_tiles, int splits, float* parts, hipStream_t s);
+int window_bwd_f32(const WindowArgs& a, int dq_splits, float* part_dq, int cut_tiles, int splits, float* parts, hipStream_t s);
 
 struct WindowSeq {
   int pos0, k_len;

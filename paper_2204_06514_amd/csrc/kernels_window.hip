@@ -68,11 +68,20 @@ __global__ __launch_bounds__(256) void window_join_kernel(WindowArgs a, int spli
   const float L = wave_sum(mine.y * weight);
   float acc[2] = {0.f, 0.f};
   const int d0 = min(lane, a.dh - 1), d1 = min(lane + 64, a.dh - 1);
-#pragma unroll 8
-  for (int s = 0; s < splits; s++) {
-    const float w = __uint_as_float(__builtin_amdgcn_readlane(__float_as_uint(weight), s));
-    acc[0] = fmaf(o[(long long)s * a.dh + d0], w, acc[0]);
-    acc[1] = fmaf(o[(long long)s * a.dh + d1], w, acc[1]);
+  for (int s0 = 0; s0 < splits; s0 += 8) {  // (beyond the last part: loads of the last)
+    float x[8][2];
+#pragma unroll
+    for (int k = 0; k < 8; k++) {
+      const float* p = o + (long long)min(s0 + k, splits - 1) * a.dh;
+      x[k][0] = p[d0];
+      x[k][1] = p[d1];
+    }
+#pragma unroll
+    for (int k = 0; k < 8; k++) {
+      const float w = __uint_as_float(__builtin_amdgcn_readlane(__float_as_uint(weight), s0 + k));
+      acc[0] = s0 + k < splits ? fmaf(x[k][0], w, acc[0]) : acc[0];
+      acc[1] = s0 + k < splits ? fmaf(x[k][1], w, acc[1]) : acc[1];
+    }
   }
   if (__any(!(fabsf(acc[0]) <= 3.4028235e38f) || !(fabsf(acc[1]) <= 3.4028235e38f)) || !(L <= 3.4028235e38f)) {
     window_fwd_row<2, T>(a, b, i, h, lane);
@@ -89,10 +98,44 @@ __global__ __launch_bounds__(256) void window_join_kernel(WindowArgs a, int spli
   if (lane == 0 && a.lse) a.lse[((long long)b * a.H + h) * a.Sq + i] = none ? -INFINITY : M * unit + logf(L);
 }
 
-// The parts of the sink tiles' keys, added in order: one wavefront to a key.
+// dQ of cut rows: the parts added in order, one wavefront to a row.  part_ds: the parts of delta (NULL: it is there already).
+template <typename T>
+__global__ __launch_bounds__(256) void window_fold_dq_kernel(WindowArgs a, int splits, const float* __restrict__ part_dq, const float* __restrict__ part_ds) {
+  const long long row = (long long)blockIdx.x * 4 + (threadIdx.x >> 6), rows = (long long)a.B * a.Hkv * a.Sq * a.group;
+  if (row >= rows) return;
+  const int lane = threadIdx.x & 63;
+  const long long per_head = (long long)a.Sq * a.group;
+  const int bh = (int)(row / per_head), r = (int)(row % per_head);
+  const int b = bh / a.Hkv, i = r / a.group, h = bh % a.Hkv * a.group + r % a.group;
+  const float* o = part_dq + row * splits * a.dh;
+  if (part_ds) {
+    const float delta = wave_sum(lane < splits ? part_ds[row * splits + lane] : 0.f);
+    if (lane == 0) a.delta[((long long)b * a.H + h) * a.Sq + i] = delta;
+  }
+  float acc[2] = {0.f, 0.f};
+  const int d0 = min(lane, a.dh - 1), d1 = min(lane + 64, a.dh - 1);
+#pragma unroll 8
+  for (int s = 0; s < splits; s++) {
+    acc[0] += o[(long long)s * a.dh + d0];
+    acc[1] += o[(long long)s * a.dh + d1];
+  }
+  if (sizeof(T) == 2 && __any(acc[0] * 0.f + acc[1] * 0.f != 0.f)) {  // (the fp32 kernels keep masked rows out of their sums)
+    __threadfence();
+    window_dq_row<2, T>(a, b, i, h, lane);
+    return;
+  }
+  T* out = strided_row((T*)a.dq, a.sq, b, i, h);
+#pragma unroll
+  for (int k = 0; k < 2; k++) {
+    const int d = lane + 64 * k;
+    if (d < a.dh) out[d] = from_f<T>(acc[k] * a.scale);
+  }
+}
+
+// The parts of the cut tiles' keys, added in order: one wavefront to a key.
 template <typename T>
 __global__ __launch_bounds__(256) void window_fold_kernel(WindowArgs a, KeyGrid kg, int tile_keys, const float* __restrict__ parts) {
-  const int keys = kg.sink_tiles * tile_keys, n = min(keys, a.Sk);
+  const int keys = kg.cut_tiles * tile_keys, n = min(keys, a.Sk);
   const int item = blockIdx.x * 4 + (threadIdx.x >> 6), lane = threadIdx.x & 63;
   if (item >= n * a.B * a.Hkv) return;
   const int j = item % n, bh = item / n;
@@ -128,45 +171,52 @@ static bool strides_fit(const FaxStrides& s, int unit) { return s.batch % unit =
 static WindowPlan window_plan(const FaxWindowDims& d) {
   WindowPlan p = {};
   p.form = FAX_ATTENTION_SCALAR;
-  p.fwd_waves = p.dq_waves = p.kv_waves = 4;
-  p.fwd_splits = p.sink_splits = 1;
+  p.waves = 1;
+  p.row_splits = p.kv_splits = 1;
   const int unit = d.dtype == FAX_F32 ? 4 : 8;
   const long long heads = (long long)d.B * d.Hkv, rows = (long long)d.Sq * (d.H / d.Hkv);
   if (d.dh % unit == 0 && d.dh <= 128 && strides_fit(d.q, unit) && strides_fit(d.kv, unit) && strides_fit(d.ctx, unit) && rows < (1 << 30)) {
     const bool f32 = d.dtype == FAX_F32;
     p.form = f32 ? FAX_ATTENTION_F32 : d.dh == 64 || d.dh == 128 ? FAX_ATTENTION_MFMA : FAX_ATTENTION_EDGE;
-    const long long t128 = (rows + 127) / 128 * heads, t32 = (rows + 31) / 32 * heads;
-    const bool few = t128 < 256;
-    if (!f32) p.fwd_waves = p.dq_waves = few ? 1 : 4;
-    // tiles of keys that a row meets: a run of them is at least two
-    const long long seen = (long long)d.window + d.sinks + 128 < d.Sk ? d.window + d.sinks + 128 : d.Sk;
-    const long long key_tiles = (seen + 63) / 64;
-    if ((few || f32) && t32 < 512) {
-      long long splits = 512 / t32;
-      if (splits > key_tiles / 2) splits = key_tiles / 2;
-      if (splits > 64) splits = 64;  // (a lane of the joining wavefront each)
-      p.fwd_splits = splits > 1 ? (int)splits : 1;
-    }
-    if (!f32 && (d.Sk + window_dkv_keys(d.dh, 4) - 1) / window_dkv_keys(d.dh, 4) * heads < 256) p.kv_waves = 1;
-    p.kv_keys = f32 ? 32 : window_dkv_keys(d.dh, p.kv_waves);
+    p.waves = !f32 && rows > 32 ? 4 : 1;
+    const long long blocks = (rows + 32 * p.waves - 1) / (32 * p.waves) * heads;
+    // Streams are cut where there are fewer than two workgroups to a CU, into parts of at least two tiles.
+    auto cut = [](long long blocks, long long tiles) {
+      long long n = blocks < 512 ? 512 / blocks : 1;
+      if (n > tiles / 2) n = tiles / 2;
+      if (n > 64) n = 64;  // (a lane of the joining wavefront each)
+      return n > 1 ? (int)n : 1;
+    };
+    const long long seen = (long long)d.window + d.sinks + 128 < d.Sk ? d.window + d.sinks + 128 : d.Sk;  // keys that a row's workgroup meets
+    p.row_splits = cut(blocks, (seen + 63) / 64);
+    p.kv_keys = f32 ? 32 : window_dkv_keys(d.dh);
     const int n = (d.Sk + p.kv_keys - 1) / p.kv_keys, sinks = d.sinks < d.Sk ? d.sinks : d.Sk;
-    p.sink_tiles = (sinks + p.kv_keys - 1) / p.kv_keys;
-    const long long usual = (long long)d.window + p.kv_keys + 64;
-    if (p.sink_tiles > 0 && 2 * p.sink_tiles <= n && d.Sq > usual) p.sink_splits = (int)(d.Sq / usual + 1 < 32 ? d.Sq / usual + 1 : 32);
-    if (p.sink_splits == 1) p.sink_tiles = 0;
+    const long long usual = (long long)d.window + p.kv_keys + 64;  // queries that see a tile without sinks
+    p.cut_tiles = (sinks + p.kv_keys - 1) / p.kv_keys;
+    if (p.cut_tiles > 0 && 2 * p.cut_tiles <= n && d.Sq > usual) p.kv_splits = (int)(d.Sq / usual + 1 < 32 ? d.Sq / usual + 1 : 32);
+    const int all = cut(n * heads, ((d.Sq < usual ? d.Sq : usual) + 63) / 64 * (d.H / d.Hkv));
+    if (all > 1) {
+      p.cut_tiles = n;
+      if (all > p.kv_splits) p.kv_splits = all;
+    }
+    if (p.kv_splits == 1) p.cut_tiles = 0;
   }
   size_t o = 0;
   auto take = [&](size_t bytes) { const size_t r = o; o += (bytes + 255) / 256 * 256; return r; };
   // forward pass and backward pass take turns in the workspace
   const size_t all_rows = (size_t)d.B * d.H * d.Sq;
-  if (p.fwd_splits > 1) {
-    p.part_o = take(all_rows * p.fwd_splits * d.dh * 4);
-    p.part_ml = take(all_rows * p.fwd_splits * 8);
+  if (p.row_splits > 1) {
+    p.part_o = take(all_rows * p.row_splits * d.dh * 4);
+    p.part_ml = take(all_rows * p.row_splits * 8);
   }
   const size_t fwd = o;
   o = 0;
   p.delta = take(all_rows * 4);
-  if (p.sink_splits > 1) p.parts = take((size_t)p.sink_splits * heads * p.sink_tiles * p.kv_keys * 2 * d.dh * 4);
+  if (p.row_splits > 1) {
+    p.part_dq = take(all_rows * p.row_splits * d.dh * 4);
+    p.part_ds = take(all_rows * p.row_splits * 4);
+  }
+  if (p.kv_splits > 1) p.parts = take((size_t)p.kv_splits * heads * p.cut_tiles * p.kv_keys * 2 * d.dh * 4);
   p.total = o > fwd ? o : fwd;
   return p;
 }
@@ -174,8 +224,8 @@ size_t window_ws_bytes(const FaxWindowDims& d) { return window_plan(d).total; }
 void window_route(const FaxWindowDims& d, FaxWindowRoute* out) {
   const WindowPlan p = window_plan(d);
   out->form = p.form;
-  out->fwd_waves = p.fwd_waves; out->fwd_splits = p.fwd_splits; out->dq_waves = p.dq_waves; out->kv_waves = p.kv_waves;
-  out->sink_splits = p.sink_splits;
+  out->waves = p.waves; out->row_splits = p.row_splits; out->kv_splits = p.kv_splits;
+  out->cut_keys = p.cut_tiles * p.kv_keys;
 }
 static bool on16(std::initializer_list<const void*> p) {
   uintptr_t all = 0;
@@ -211,13 +261,13 @@ int window_fwd(const FaxWindowDims& d, const void* q, const void* k, const void*
   } else {
     float* part_o = (float*)(w + p.part_o);
     float2* part_ml = (float2*)(w + p.part_ml);
-    if (p.form == FAX_ATTENTION_F32) FAX_TRY(window_fwd_f32(a, p.fwd_splits, part_o, part_ml, s));
-    else FAX_TRY(window_fwd_mfma(a, p.fwd_waves, p.fwd_splits, part_o, part_ml, s));
-    if (p.fwd_splits > 1) {
+    if (p.form == FAX_ATTENTION_F32) FAX_TRY(window_fwd_f32(a, p.row_splits, part_o, part_ml, s));
+    else FAX_TRY(window_fwd_mfma(a, p.waves, p.row_splits, part_o, part_ml, s));
+    if (p.row_splits > 1) {
       const float log2e = 1.4426950408889634f;
       const dim3 grid((unsigned)(((long long)a.B * a.H * a.Sq + 3) / 4));
-      if (d.dtype == FAX_F32) hipLaunchKernelGGL(window_join_kernel<float>, grid, dim3(256), 0, s, a, p.fwd_splits, part_o, part_ml, log2e, 1.f);
-      else hipLaunchKernelGGL(window_join_kernel<bf16_t>, grid, dim3(256), 0, s, a, p.fwd_splits, part_o, part_ml, a.scale * log2e, a.scale);
+      if (d.dtype == FAX_F32) hipLaunchKernelGGL(window_join_kernel<float>, grid, dim3(256), 0, s, a, p.row_splits, part_o, part_ml, log2e, 1.f);
+      else hipLaunchKernelGGL(window_join_kernel<bf16_t>, grid, dim3(256), 0, s, a, p.row_splits, part_o, part_ml, a.scale * log2e, a.scale);
     }
   }
   FAX_LAUNCH_CHECK("window_attention_fwd");
@@ -237,18 +287,21 @@ int window_bwd(const FaxWindowDims& d, const void* q, const void* k, const void*
     FAX_TRY(rows_launch<1>(a, d.dtype, s));
     FAX_TRY(rows_launch<2>(a, d.dtype, s));
   } else {
-    float* parts = (float*)(w + p.parts);
+    float *parts = (float*)(w + p.parts), *part_dq = (float*)(w + p.part_dq), *part_ds = (float*)(w + p.part_ds);
+    const unsigned row_blocks = (unsigned)(((long long)a.B * a.H * a.Sq + 3) / 4);
     if (p.form == FAX_ATTENTION_F32) {
       FAX_TRY(rows_launch<3>(a, d.dtype, s));
-      FAX_TRY(window_bwd_f32(a, p.sink_tiles, p.sink_splits, parts, s));
+      FAX_TRY(window_bwd_f32(a, p.row_splits, part_dq, p.cut_tiles, p.kv_splits, parts, s));
+      if (p.row_splits > 1) hipLaunchKernelGGL(window_fold_dq_kernel<float>, dim3(row_blocks), dim3(256), 0, s, a, p.row_splits, part_dq, (const float*)nullptr);
     } else {
       // dQ first: it also leaves delta, which dK and dV need
-      FAX_TRY(window_dq_mfma(a, p.dq_waves, s));
-      FAX_TRY(window_dkv_mfma(a, p.kv_waves, p.sink_tiles, p.sink_splits, parts, s));
+      FAX_TRY(window_dq_mfma(a, p.waves, p.row_splits, part_dq, part_ds, s));
+      if (p.row_splits > 1) hipLaunchKernelGGL(window_fold_dq_kernel<bf16_t>, dim3(row_blocks), dim3(256), 0, s, a, p.row_splits, part_dq, part_ds);
+      FAX_TRY(window_dkv_mfma(a, p.cut_tiles, p.kv_splits, parts, s));
     }
-    if (p.sink_splits > 1) {
-      const KeyGrid kg(a, p.kv_keys, p.sink_tiles, p.sink_splits);
-      const long long keys = (long long)(p.sink_tiles * p.kv_keys < a.Sk ? p.sink_tiles * p.kv_keys : a.Sk) * a.B * a.Hkv;
+    if (p.kv_splits > 1) {
+      const KeyGrid kg(a, p.kv_keys, p.cut_tiles, p.kv_splits);
+      const long long keys = (long long)(p.cut_tiles * p.kv_keys < a.Sk ? p.cut_tiles * p.kv_keys : a.Sk) * a.B * a.Hkv;
       const dim3 grid((unsigned)((keys + 3) / 4));
       if (d.dtype == FAX_F32) hipLaunchKernelGGL(window_fold_kernel<float>, grid, dim3(256), 0, s, a, kg, p.kv_keys, parts);
       else hipLaunchKernelGGL(window_fold_kernel<bf16_t>, grid, dim3(256), 0, s, a, kg, p.kv_keys, parts);

@@ -4,6 +4,8 @@
 
 namespace fax {
 
+static constexpr int WPG = 4;  // wavefronts of a workgroup, which share the streamed tiles: a tile for each would leave room for two on a CU
+
 // What both forms have in common: the stream of query tiles and its loads.
 template <int DH, int WAVES, bool SWZ16, bool EDGE>
 struct QueryStream {
@@ -54,7 +56,7 @@ struct QueryStream {
 // ---------------------------------------------------------------------------------------------
 // 32 keys to a wave.  Per 32-query half: S = Q K^T and dP = dO V^T, P and dS, dV^T += dO^T P and dK^T += Q^T dS.
 // ---------------------------------------------------------------------------------------------
-template <int DW, bool EDGE, int WPG>
+template <int DW, bool EDGE>
 __global__ __launch_bounds__(64 * WPG, 2) void window_dkv_mfma_kernel(WindowArgs a, KeyGrid kg, float* __restrict__ parts) {
   constexpr int DH = row_width<DW>();
   typedef QueryStream<DH, WPG, false, EDGE> Stream;
@@ -68,7 +70,7 @@ __global__ __launch_bounds__(64 * WPG, 2) void window_dkv_mfma_kernel(WindowArgs
   const int b = it_.bh / a.Hkv, hk = it_.bh % a.Hkv;
   const WindowSeq sq(a, b);
   const int lane = threadIdx.x & 63, g = lane >> 5;
-  const int wave = WPG == 1 ? 0 : __builtin_amdgcn_readfirstlane(threadIdx.x >> 6);
+  const int wave = __builtin_amdgcn_readfirstlane(threadIdx.x >> 6);
   const int hw = EDGE ? a.dh : DW, nch = hw / 8;
   const float scale = a.scale, c = scale * LOG2E;
   if (EDGE) clear_lds(smem, 2 * Stream::STAGE);
@@ -196,7 +198,7 @@ __global__ __launch_bounds__(64 * WPG, 2) void window_dkv_mfma_kernel(WindowArgs
   }
 
   if (it_.split >= 0) {
-    float* o = part_row(a, kg, parts, it_.split, it_.bh, kg.sink_tiles * RT, jk);
+    float* o = part_row(a, kg, parts, it_.split, it_.bh, kg.cut_tiles * RT, jk);
 #pragma unroll
     for (int dt = 0; dt < DT; dt++)
 #pragma unroll
@@ -225,7 +227,7 @@ __global__ __launch_bounds__(64 * WPG, 2) void window_dkv_mfma_kernel(WindowArgs
 // ---------------------------------------------------------------------------------------------
 // 16 keys to a wave (head widths above 64).
 // ---------------------------------------------------------------------------------------------
-template <int DW, bool EDGE, int WPG>
+template <int DW, bool EDGE>
 __global__ __launch_bounds__(64 * WPG, 2) void window_dkv16_mfma_kernel(WindowArgs a, KeyGrid kg, float* __restrict__ parts) {
   constexpr int DH = row_width<DW>();
   typedef QueryStream<DH, WPG, true, EDGE> Stream;
@@ -239,7 +241,7 @@ __global__ __launch_bounds__(64 * WPG, 2) void window_dkv16_mfma_kernel(WindowAr
   const int b = it_.bh / a.Hkv, hk = it_.bh % a.Hkv;
   const WindowSeq sq(a, b);
   const int lane = threadIdx.x & 63, gq = lane >> 4;
-  const int wave = WPG == 1 ? 0 : __builtin_amdgcn_readfirstlane(threadIdx.x >> 6);
+  const int wave = __builtin_amdgcn_readfirstlane(threadIdx.x >> 6);
   const int hw = EDGE ? a.dh : DW, nch = hw / 8;
   const float scale = a.scale, c = scale * LOG2E;
   if (EDGE) clear_lds(smem, 2 * Stream::STAGE);
@@ -368,7 +370,7 @@ __global__ __launch_bounds__(64 * WPG, 2) void window_dkv16_mfma_kernel(WindowAr
   }
 
   if (it_.split >= 0) {
-    float* o = part_row(a, kg, parts, it_.split, it_.bh, kg.sink_tiles * RT, jk);
+    float* o = part_row(a, kg, parts, it_.split, it_.bh, kg.cut_tiles * RT, jk);
 #pragma unroll
     for (int dt = 0; dt < DT; dt++) {
       const int d = dt * 16 + gq * 4;
@@ -404,27 +406,22 @@ __global__ __launch_bounds__(64 * WPG, 2) void window_dkv16_mfma_kernel(WindowAr
   }
 }
 
-int window_dkv_keys(int dh, int waves) { return (dh <= 64 ? 32 : 16) * waves; }
+int window_dkv_keys(int dh) { return (dh <= 64 ? 32 : 16) * WPG; }
 
-int window_dkv_mfma(const WindowArgs& a, int waves, int sink_tiles, int splits, float* parts, hipStream_t s) {
-  const int keys = window_dkv_keys(a.dh, waves), heads = a.B * a.Hkv;
-  const KeyGrid kg(a, keys, sink_tiles, splits);
-  const unsigned grid = kg.blocks(heads);
+int window_dkv_mfma(const WindowArgs& a, int cut_tiles, int splits, float* parts, hipStream_t s) {
+  const KeyGrid kg(a, window_dkv_keys(a.dh), cut_tiles, splits);
+  const unsigned grid = kg.blocks(a.B * a.Hkv);
   auto launch = [&](auto kern, size_t row) -> int {
     const size_t lds = 2 * (2 * (size_t)TR * row * 2 + 4 * 256);
     FAX_HIP(hipFuncSetAttribute(reinterpret_cast<const void*>(kern), hipFuncAttributeMaxDynamicSharedMemorySize, (int)lds));
-    hipLaunchKernelGGL(kern, dim3(grid), dim3(64 * waves), lds, s, a, kg, parts);
+    hipLaunchKernelGGL(kern, dim3(grid), dim3(64 * WPG), lds, s, a, kg, parts);
     return FAX_OK;
   };
-  auto go = [&](auto wpg) -> int {
-    constexpr int W = decltype(wpg)::value;
-    if (a.dh == 64) return launch(window_dkv_mfma_kernel<64, false, W>, 64);
-    if (a.dh == 128) return launch(window_dkv16_mfma_kernel<128, false, W>, 128);
-    if (a.dh < 64) return launch(window_dkv_mfma_kernel<64, true, W>, 64);
-    if (a.dh <= 96) return launch(window_dkv16_mfma_kernel<96, true, W>, 128);
-    return launch(window_dkv16_mfma_kernel<128, true, W>, 128);
-  };
-  return waves == 1 ? go(I<1>{}) : go(I<4>{});
+  if (a.dh == 64) return launch(window_dkv_mfma_kernel<64, false>, 64);
+  if (a.dh == 128) return launch(window_dkv16_mfma_kernel<128, false>, 128);
+  if (a.dh < 64) return launch(window_dkv_mfma_kernel<64, true>, 64);
+  if (a.dh <= 96) return launch(window_dkv16_mfma_kernel<96, true>, 128);
+  return launch(window_dkv16_mfma_kernel<128, true>, 128);
 }
 
 }  // namespace fax

@@ -132,8 +132,8 @@ __global__ __launch_bounds__(256, 2) void window_fwd_f32_kernel(WindowArgs a, in
 
 // Both halves of the backward pass in one launch, delta given: the first `kv_blocks` workgroups have keys (dK, dV), the others rows (dQ).
 template <int DH, bool EXACT>
-__global__ __launch_bounds__(256, DH > 64 ? 1 : 2) void window_bwd_f32_kernel(WindowArgs a, KeyGrid kg, int kv_blocks, int n_tiles, int items,
-                                                                           float* __restrict__ parts) {
+__global__ __launch_bounds__(256, DH > 64 ? 1 : 2) void window_bwd_f32_kernel(WindowArgs a, KeyGrid kg, int kv_blocks, int n_tiles, int items, int dq_splits,
+                                                                           float* __restrict__ part_dq, float* __restrict__ parts) {
   extern __shared__ __attribute__((aligned(16))) float smem_a[];
   const int lane = threadIdx.x & 63, l31 = lane & 31, h = lane >> 5, dh = a.dh;
   const int wave = __builtin_amdgcn_readfirstlane(threadIdx.x >> 6);
@@ -141,8 +141,10 @@ __global__ __launch_bounds__(256, DH > 64 ? 1 : 2) void window_bwd_f32_kernel(Wi
   float* slot = smem_a + wave * slot_floats<DH>();
 
   if ((int)blockIdx.x >= kv_blocks) {
-    const int item = xcd_item(blockIdx.x - kv_blocks, gridDim.x - kv_blocks);
+    int item = xcd_item(blockIdx.x - kv_blocks, gridDim.x - kv_blocks);
     if (item >= items) return;
+    const int split = item % dq_splits;
+    item /= dq_splits;
     const int bh = item / n_tiles, b = bh / a.Hkv, hk = bh % a.Hkv, row0 = item % n_tiles * 32, rows = a.Sq * a.group;
     const WindowSeq sq(a, b);
     const HeadTile<DH, EXACT> Kt{strided_row((const float*)a.k, a.skv, b, 0, hk), (int)a.skv.row, sq.k_len, dh};
@@ -157,7 +159,8 @@ __global__ __launch_bounds__(256, DH > 64 ? 1 : 2) void window_bwd_f32_kernel(Wi
     const KeyTiles<F32_TILE> kt(KeyRanges(a, sq, p0, p1));
     f32x16 dq[DH / 32];
     zero<DH>(dq);
-    for (int u = wave; u < kt.n; u += 4) {
+    const int u1 = (int)((long long)kt.n * (split + 1) / dq_splits);
+    for (int u = (int)((long long)kt.n * split / dq_splits) + wave; u < u1; u += 4) {
       const int j0 = kt.key(u);
       float4 kf[DH / 8], vf[DH / 8];
       float kc[16][DH / 32];
@@ -185,6 +188,10 @@ __global__ __launch_bounds__(256, DH > 64 ? 1 : 2) void window_bwd_f32_kernel(Wi
       for (int w = 1; w < 4; w++) {
         const float4 y = *reinterpret_cast<const float4*>(smem_a + w * slot_floats<DH>() + row * (DH + 4) + col);
         x.x += y.x; x.y += y.y; x.z += y.z; x.w += y.w;
+      }
+      if (dq_splits > 1) {
+        *reinterpret_cast<float4*>(part_dq + (((long long)bh * rows + rr) * dq_splits + split) * dh + col) = x;
+        continue;
       }
       const int ii = rr / a.group;
       *reinterpret_cast<float4*>(strided_row((float*)a.dq, a.sq, b, ii, hk * a.group + rr - ii * a.group) + col) =
@@ -249,7 +256,7 @@ __global__ __launch_bounds__(256, DH > 64 ? 1 : 2) void window_bwd_f32_kernel(Wi
   int ld = (int)a.skv.row, rows = keys;
   float mul = a.scale;
   if (it.split >= 0) {
-    ko = part_row(a, kg, parts, it.split, it.bh, kg.sink_tiles * F32_TILE, k0);
+    ko = part_row(a, kg, parts, it.split, it.bh, kg.cut_tiles * F32_TILE, k0);
     vo = ko + dh;
     ld = 2 * dh;
     rows = F32_TILE;
@@ -296,17 +303,17 @@ int window_fwd_f32(const WindowArgs& a, int splits, float* part_o, void* part_ml
   });
 }
 
-int window_bwd_f32(const WindowArgs& a, int sink_tiles, int splits, float* parts, hipStream_t s) {
+int window_bwd_f32(const WindowArgs& a, int dq_splits, float* part_dq, int cut_tiles, int splits, float* parts, hipStream_t s) {
   const int n_tiles = (int)(((long long)a.Sq * a.group + 31) / 32), heads = a.B * a.Hkv;
-  const long long items = (long long)n_tiles * heads;
-  const KeyGrid kg(a, F32_TILE, sink_tiles, splits);
+  const long long items = (long long)n_tiles * heads * dq_splits;
+  const KeyGrid kg(a, F32_TILE, cut_tiles, splits);
   const unsigned kv_blocks = kg.blocks(heads);
   return by_width(a.dh, [&](auto dw, auto exact) -> int {
     constexpr int DH = decltype(dw)::value;
     auto kern = window_bwd_f32_kernel<DH, decltype(exact)::value>;
     constexpr int lds = 4 * slot_floats<DH>() * (int)sizeof(float);
     FAX_HIP(hipFuncSetAttribute(reinterpret_cast<const void*>(kern), hipFuncAttributeMaxDynamicSharedMemorySize, lds));
-    hipLaunchKernelGGL(kern, dim3(kv_blocks + xcd_grid(items)), dim3(256), lds, s, a, kg, (int)kv_blocks, n_tiles, (int)items, parts);
+    hipLaunchKernelGGL(kern, dim3(kv_blocks + xcd_grid(items)), dim3(256), lds, s, a, kg, (int)kv_blocks, n_tiles, (int)items, dq_splits, part_dq, parts);
     return FAX_OK;
   });
 }

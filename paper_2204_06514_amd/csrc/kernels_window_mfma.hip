@@ -209,16 +209,19 @@ __global__ __launch_bounds__(64 * WPG, 2) void window_fwd_mfma_kernel(WindowArgs
 // ---------------------------------------------------------------------------------------------
 // dQ, and delta = dctx . ctx by row.  The same tiles; per 32-key half S^T = K Q^T and dP^T = V dO^T, dS^T = P^T (dP^T - delta), dQ^T += K^T dS^T.
 // ---------------------------------------------------------------------------------------------
-template <int DW, bool EDGE, int WPG>
-__global__ __launch_bounds__(64 * WPG, 2) void window_dq_mfma_kernel(WindowArgs a, int n_tiles, int items) {
+template <int DW, bool EDGE, int WPG, bool PART>
+__global__ __launch_bounds__(64 * WPG, 2) void window_dq_mfma_kernel(WindowArgs a, int n_tiles, int items, int splits, float* __restrict__ part_dq,
+                                                                     float* __restrict__ part_ds) {
   constexpr int DH = row_width<DW>();
   constexpr int KS = DW / 16, DT = DW / 32, TB = TR * DH * 2;
   constexpr int N1 = 2 * KS, N3 = 2 * DT, LEAD = N3;
   constexpr int NSEG = DH / 8 / WPG;
   static_assert(N1 % LEAD == 0, "slot plan");
   extern __shared__ __attribute__((aligned(16))) char smem[];
-  const int item = xcd_item(blockIdx.x, gridDim.x);
+  int item = xcd_item(blockIdx.x, gridDim.x);
   if (item >= items) return;
+  int split = 0;
+  if (PART) { split = item % splits; item /= splits; }
   const int tile_no = item % n_tiles, bh = item / n_tiles;
   const int b = bh / a.Hkv, hk = bh % a.Hkv;
   const WindowSeq sq(a, b);
@@ -231,6 +234,7 @@ __global__ __launch_bounds__(64 * WPG, 2) void window_dq_mfma_kernel(WindowArgs 
   const unsigned sm = lds_addr(smem);
   if (EDGE) clear_lds(smem, 4 * TB);
   const KeyTiles<TR> kt(KeyRanges(a, sq, rt.p0, rt.p1));
+  const int u0 = PART ? (int)((long long)kt.n * split / splits) : 0, u1 = PART ? (int)((long long)kt.n * (split + 1) / splits) : kt.n;
 
   bf16x8 qf[KS], dof[KS];
   const bf16_t* qp = strided_row((const bf16_t*)a.q, a.sq, b, rt.i, rt.h);
@@ -323,35 +327,50 @@ __global__ __launch_bounds__(64 * WPG, 2) void window_dq_mfma_kernel(WindowArgs 
     __builtin_amdgcn_s_setprio(0);
   };
 
-  if (kt.n > 0) {
-    load(kt.key(0), 0);
+  if (u0 < u1) {
+    load(kt.key(u0), 0);
     lds_dma_wait();
     __syncthreads();
     // Runs of tiles that take the masks (or that no row of the wave sees) and of tiles that do not, in loops of their own: one loop over both kinds
     // keeps the accumulators in two places, which does not fit the registers.
     auto full = [&](int u) { return sees_all(a, sq.k_len, rt.wp0, rt.wp1, kt.key(u), TR); };
     auto next = [&](int u) __attribute__((always_inline)) {
-      if (u + 1 < kt.n) load(kt.key(u + 1), (u + 1) & 1);
+      if (u + 1 < u1) load(kt.key(u + 1), (u - u0 + 1) & 1);
     };
     auto done = [&]() {
       lds_dma_wait();
       __syncthreads();
     };
-    for (int u = 0; u < kt.n;) {
-      for (; u < kt.n && !full(u); u++) {
+    for (int u = u0; u < u1;) {
+      for (; u < u1 && !full(u); u++) {
         next(u);
-        if (sees_any(a, sq.k_len, rt.wp0, rt.wp1, kt.key(u), TR)) tile(T_{}, kt.key(u), (u) & 1);
+        if (sees_any(a, sq.k_len, rt.wp0, rt.wp1, kt.key(u), TR)) tile(T_{}, kt.key(u), (u - u0) & 1);
         done();
       }
-      for (; u < kt.n && full(u); u++) {
+      for (; u < u1 && full(u); u++) {
         next(u);
-        tile(F_{}, kt.key(u), (u) & 1);
+        tile(F_{}, kt.key(u), (u - u0) & 1);
         done();
       }
     }
   }
   // The probabilities of a row add up to one, so the sum of its dS is what delta, formed from ctx as it was rounded, lacks: dK gets it with that.
-  di += sum32(ds_sum);
+  ds_sum = sum32(ds_sum);
+  if (PART) {
+    if (!rt.ok) return;
+    const long long at = ((long long)bh * rt.rows + rt.row) * splits + split;
+    if (g == 0) part_ds[at] = split == 0 ? di + ds_sum : ds_sum;
+    float* o = part_dq + at * a.dh;
+#pragma unroll
+    for (int dt = 0; dt < DT; dt++)
+#pragma unroll
+      for (int q = 0; q < 4; q++) {
+        const int d = dt * 32 + q * 8 + g * 4;
+        if (!EDGE || dt * 32 + q * 8 < hw) *reinterpret_cast<float4*>(o + d) = make_float4(dq[dt][q * 4], dq[dt][q * 4 + 1], dq[dt][q * 4 + 2], dq[dt][q * 4 + 3]);
+      }
+    return;
+  }
+  di += ds_sum;
   if (g == 0 && rt.ok) a.delta[stat] = di;
   const unsigned long long odd = __builtin_amdgcn_ballot_w64(rt.ok && not_finite(dq, 0.f) != 0.f);
   unsigned again = (unsigned)odd | (unsigned)(odd >> 32);
@@ -397,20 +416,21 @@ int window_fwd_mfma(const WindowArgs& a, int waves, int splits, float* part_o, v
   });
 }
 
-int window_dq_mfma(const WindowArgs& a, int waves, hipStream_t s) {
+int window_dq_mfma(const WindowArgs& a, int waves, int splits, float* part_dq, float* part_ds, hipStream_t s) {
   const int n_tiles = (int)(((long long)a.Sq * a.group + 32 * waves - 1) / (32 * waves));
-  const long long items = (long long)n_tiles * a.B * a.Hkv;
+  const long long items = (long long)n_tiles * a.B * a.Hkv * splits;
   return by_width(a.dh, [&](auto dw, auto edge) -> int {
     constexpr int DW = decltype(dw)::value;
     constexpr bool E = decltype(edge)::value;
     constexpr size_t lds = 4 * (size_t)TR * row_width<DW>() * 2;
-    auto go = [&](auto wpg) -> int {
-      auto kern = window_dq_mfma_kernel<DW, E, decltype(wpg)::value>;
+    auto go = [&](auto wpg, auto part) -> int {
+      auto kern = window_dq_mfma_kernel<DW, E, decltype(wpg)::value, decltype(part)::value>;
       FAX_TRY(set_lds(kern, lds));
-      hipLaunchKernelGGL(kern, dim3(xcd_grid(items)), dim3(64 * waves), lds, s, a, n_tiles, (int)items);
+      hipLaunchKernelGGL(kern, dim3(xcd_grid(items)), dim3(64 * waves), lds, s, a, n_tiles, (int)items, splits, part_dq, part_ds);
       return FAX_OK;
     };
-    return waves == 1 ? go(I<1>{}) : go(I<4>{});
+    if (splits > 1) return waves == 1 ? go(I<1>{}, T_{}) : go(I<4>{}, T_{});
+    return waves == 1 ? go(I<1>{}, F_{}) : go(I<4>{}, F_{});
   });
 }
 

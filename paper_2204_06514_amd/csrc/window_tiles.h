@@ -32,40 +32,40 @@ __device__ __forceinline__ bool sees_any(const WindowArgs& a, int k_len, int p0,
 }
 
 // dK and dV.  A workgroup has a tile of keys of one key head and streams the tiles of queries of all its query heads that see some of
-// them, head by head.  Keys among the sinks are seen by every later query, not by a window's length of them: their tiles' streams are cut into
-// `splits` parts, workgroups of their own that leave sums for window_fold_kernel.  They are the first workgroups of the launch; the other
-// tiles follow.
+// them, head by head.  The streams of the first `cut_tiles` tiles are cut into `splits` parts, workgroups of their own that leave sums for
+// window_fold_kernel: those of the sinks, which every later query sees and not a window's length of them, or of all, where tiles are few.
+// They are the first workgroups of the launch; the other tiles follow.
 struct KeyGrid {
-  int n_tiles, sink_tiles, splits, sink_blocks;  // key tiles of a head; how many of them are split, into how many parts; workgroups of those
-  KeyGrid(const WindowArgs& a, int keys, int sink_tiles_, int splits_) {
+  int n_tiles, cut_tiles, splits, cut_blocks;  // key tiles of a head; how many of them are cut, into how many parts; workgroups of those
+  KeyGrid(const WindowArgs& a, int keys, int cut_tiles_, int splits_) {
     n_tiles = (a.Sk + keys - 1) / keys;
-    sink_tiles = splits_ > 1 ? sink_tiles_ : 0;
+    cut_tiles = splits_ > 1 ? cut_tiles_ : 0;
     splits = splits_;
-    sink_blocks = (int)xcd_grid((long long)sink_tiles * a.B * a.Hkv * splits);
+    cut_blocks = (int)xcd_grid((long long)cut_tiles * a.B * a.Hkv * splits);
   }
-  unsigned blocks(int heads) const { return sink_blocks + xcd_grid((long long)(n_tiles - sink_tiles) * heads); }
+  unsigned blocks(int heads) const { return cut_blocks + xcd_grid((long long)(n_tiles - cut_tiles) * heads); }
 };
 struct KeyItem {
   int bh, tile, split;  // split < 0: whole
   bool ok;
   __device__ __forceinline__ KeyItem(const KeyGrid& k, int heads, int block, int grid) {
-    if (block < k.sink_blocks) {
+    if (block < k.cut_blocks) {
       split = block % k.splits;
       const int r = block / k.splits;
-      tile = r % max(k.sink_tiles, 1);
-      bh = r / max(k.sink_tiles, 1);
+      tile = r % max(k.cut_tiles, 1);
+      bh = r / max(k.cut_tiles, 1);
       ok = bh < heads;
     } else {
-      const int rest = k.n_tiles - k.sink_tiles, i = xcd_item(block - k.sink_blocks, grid - k.sink_blocks);
+      const int rest = k.n_tiles - k.cut_tiles, i = xcd_item(block - k.cut_blocks, grid - k.cut_blocks);
       split = -1;
       ok = i < rest * heads;
-      tile = k.sink_tiles + i % max(rest, 1);
+      tile = k.cut_tiles + i % max(rest, 1);
       bh = i / max(rest, 1);
     }
   }
 };
 
-// A part's row of scratch: [part, head, key of the sink tiles, dK | dV, feature].
+// A part's row of scratch: [part, head, key of the cut tiles, dK | dV, feature].
 __device__ __forceinline__ float* part_row(const WindowArgs& a, const KeyGrid& k, float* parts, int split, int bh, int keys, int j) {
   return parts + ((((long long)split * a.B * a.Hkv + bh) * keys + j) * 2) * a.dh;
 }

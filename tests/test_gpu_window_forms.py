@@ -1,0 +1,99 @@
+"""fax_window_attention_*: every form that its sizes can take, each at a size that takes it (fax_window_attention_route says so), against
+float64 with derived bounds."""
+import pytest
+import torch
+
+import paper_2204_06514_amd as fax
+from oracle import operators as orc
+from helpers import DEV
+from test_gpu_window import TD, both, check, make, run
+
+pytestmark = pytest.mark.gpu
+
+
+def route(B, Sq, Sk, H, Hkv, dh, dtype, window, sinks):
+    code = fax.FAX_F32 if dtype == "f32" else fax.FAX_BF16
+    return fax.fax_window_attention_route(fax.FaxWindowDims(B, Sq, Sk, H, Hkv, dh, code, window, sinks, *[fax.FaxStrides()] * 3))
+
+
+def forms(r):
+    return {n: getattr(r, n) for n, _ in r._fields_}
+
+
+# Whole workgroups of four wavefronts, in every head width class; the sinks' keys cut and not.
+@pytest.mark.parametrize("dh", [40, 64, 80, 128, 104])
+@pytest.mark.parametrize("H,Hkv", [(32, 32), (40, 10)])
+@pytest.mark.parametrize("window,sinks", [(100, 4), (2000, 130)])
+def test_four_wavefronts(dh, H, Hkv, window, sinks):
+    S = 2100 if Hkv == 32 else 1700
+    if Hkv == 10 and dh in (40, 104):
+        pytest.skip("two widths are enough for grouped heads")
+    r = route(1, S, S, H, Hkv, dh, "bf16", window, sinks)
+    assert (r.waves, r.row_splits) == (4, 1), forms(r)
+    if Hkv == 32:
+        assert (r.kv_splits > 1) == (window == 100) and r.cut_keys < S, forms(r)
+    both(1, S, S, H, Hkv, dh, "bf16", window, sinks, torch.tensor([0], dtype=torch.int32), torch.tensor([S - 70], dtype=torch.int32))
+
+
+@pytest.mark.parametrize("dtype", ["bf16", "f32"])
+@pytest.mark.parametrize("dh", [24, 64, 96, 128])
+@pytest.mark.parametrize("S,H,Hkv,window,sinks", [(700, 2, 1, 10000, 0), (900, 4, 4, 200, 3), (1500, 8, 1, 64, 70), (130, 1, 1, 130, 130)])
+def test_cut_streams(S, H, Hkv, window, sinks, dh, dtype):
+    r = route(1, S, S, H, Hkv, dh, dtype, window, sinks)
+    if S > 130:
+        assert r.row_splits > 1 or r.kv_splits > 1, forms(r)
+    if S == 700:
+        assert r.row_splits > 1 and r.kv_splits > 1 and r.cut_keys >= S, forms(r)
+    both(1, S, S, H, Hkv, dh, dtype, window, sinks)
+
+
+@pytest.mark.parametrize("dtype", ["bf16", "f32"])
+def test_sinks_alone_are_cut(dtype):
+    B, S, H, window, sinks = 6, 1400, 8, 20, 5
+    r = route(B, S, S, H, H, 64, dtype, window, sinks)
+    assert r.kv_splits > 1 and 0 < r.cut_keys < S, forms(r)
+    both(B, S, S, H, H, 64, dtype, window, sinks)
+
+
+@pytest.mark.parametrize("dtype", ["bf16", "f32"])
+@pytest.mark.parametrize("dh", [64, 80, 128])
+def test_single_tokens_of_many_caches(dh, dtype):
+    B, Sk = 40, 1030
+    k_len = torch.randint(0, Sk + 1, (B,), generator=torch.Generator().manual_seed(1), dtype=torch.int32)
+    for H, Hkv in ((8, 8), (16, 2)):
+        both(B, 1, Sk, H, Hkv, dh, dtype, 500, 4, k_len - 1, k_len, backward=False)
+
+
+def test_scalar_kernels_take_the_rest():
+    for dh, dtype in ((33, "bf16"), (136, "bf16"), (256, "f32"), (6, "f32")):
+        assert route(1, 50, 50, 2, 2, dh, dtype, 10, 0).form == fax.FAX_ATTENTION_SCALAR
+        both(1, 50, 50, 2, 2, dh, dtype, 10, 2)
+
+
+def test_offsets_beyond_32_bits():
+    """Rows, then heads and sequences so far apart that the last ones' places do not fit 32 bits, in elements or bytes."""
+    dh, apart, Sk = 64, (1 << 24) - 8, 300
+    room = torch.empty(Sk * apart, dtype=torch.bfloat16, device=DEV)  # 10 GB
+    k, v = (room.as_strided((1, Sk, 1, dh), (0, apart, 0, 1), o) for o in (0, dh))
+    q, kk, vv, d = make(1, Sk, Sk, 2, 1, dh, "bf16")
+    k.copy_(kk)
+    v.copy_(vv)
+    assert fax.fax_window_attention_route(fax.window_dims(q, k, 100, 2)).form == fax.FAX_ATTENTION_MFMA
+    dims = fax.window_dims(q.to(DEV), k, 100, 2)
+    dk, dv = (room.as_strided((1, Sk, 1, dh), (0, apart, 0, 1), o) for o in (2 * dh, 3 * dh))
+    n = fax.fax_window_attention_workspace_bytes(dims)
+    ws = torch.empty(n, dtype=torch.uint8, device=DEV)
+    qd, dd = q.to(DEV), d.to(DEV)
+    ctx, dq, lse = torch.empty_like(qd), torch.empty_like(qd), torch.empty(1, 2, Sk, device=DEV)
+    fax.fax_window_attention_fwd(dims, qd, k, v, None, None, ctx, lse, ws, n)
+    fax.fax_window_attention_bwd(dims, qd, k, v, None, None, ctx, lse, dd, dq, dk, dv, ws, n)
+    got = {"ctx": ctx, "lse": lse, "dq": dq, "dk": dk, "dv": dv}
+    check({a: b.cpu().double() for a, b in got.items()},
+          orc.window_attention(q.double(), kk.double(), vv.double(), 100, 2, None, None, d.double(), TD["bf16"]))
+    far = (2 ** 31 + 64, dh, 7 * 10 ** 8, 1)
+    k, v = (room.as_strided((2, 40, 3, dh), far, o) for o in (0, 40 * dh))
+    q, kk, vv, d = make(2, 40, 40, 6, 3, dh, "bf16", seed=1)
+    k.copy_(kk)
+    v.copy_(vv)
+    got = run(q.to(DEV), k, v, None, 9, 2, backward=False)
+    check(got, orc.window_attention(q.double(), kk.double(), vv.double(), 9, 2, dtype=TD["bf16"]))
