@@ -92,7 +92,7 @@ class FaxWindowDims(C.Structure):
 
 
 class FaxWindowRoute(C.Structure):
-    _fields_ = [(n, C.c_int32) for n in ("form", "waves", "row_splits", "kv_splits", "cut_keys")]
+    _fields_ = [(n, C.c_int32) for n in ("form", "waves", "fwd_splits", "dq_splits", "sink_splits", "key_splits")]
 
 
 class FaxAdamWTensor(C.Structure):

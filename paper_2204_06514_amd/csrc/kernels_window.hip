@@ -134,19 +134,22 @@ __global__ __launch_bounds__(256) void window_fold_dq_kernel(WindowArgs a, int s
 
 // The parts of the cut tiles' keys, added in order: one wavefront to a key.
 template <typename T>
-__global__ __launch_bounds__(256) void window_fold_kernel(WindowArgs a, KeyGrid kg, int tile_keys, const float* __restrict__ parts) {
-  const int keys = kg.cut_tiles * tile_keys, n = min(keys, a.Sk);
-  const int item = blockIdx.x * 4 + (threadIdx.x >> 6), lane = threadIdx.x & 63;
-  if (item >= n * a.B * a.Hkv) return;
-  const int j = item % n, bh = item / n;
+__global__ __launch_bounds__(256) void window_fold_kernel(WindowArgs a, KeyGrid kg, const float* __restrict__ parts) {
+  const int from = kg.fold_from(), n = kg.fold_keys(a);
+  const long long item = (long long)blockIdx.x * 4 + (threadIdx.x >> 6);
+  const int lane = threadIdx.x & 63;
+  if (item >= (long long)n * a.B * a.Hkv) return;
+  const int j = from + (int)(item % n), bh = (int)(item / n);
+  const int splits = j < kg.sink_tiles * kg.keys ? kg.sink_splits : kg.rest_splits;
   float s[4] = {0.f, 0.f, 0.f, 0.f};  // dK and dV, two 64-wide pieces each
-  for (int p = 0; p < kg.splits; p++) {
-    const float* o = part_row(a, kg, const_cast<float*>(parts), p, bh, keys, j);
-#pragma unroll
-    for (int k = 0; k < 4; k++) {
-      const int d = lane + 64 * (k & 1);
-      if (d < a.dh) s[k] += o[(k >> 1) * a.dh + d];
-    }
+  const int d0 = min(lane, a.dh - 1), d1 = min(lane + 64, a.dh - 1);
+#pragma unroll 4
+  for (int p = 0; p < splits; p++) {
+    const float* o = parts + kg.part(a, p, bh, j) * 2 * a.dh;
+    s[0] += o[d0];
+    s[1] += o[d1];
+    s[2] += o[a.dh + d0];
+    s[3] += o[a.dh + d1];
   }
   const int b = bh / a.Hkv, hk = bh % a.Hkv;
   if (__any((s[0] * 0.f + s[1] * 0.f) + (s[2] * 0.f + s[3] * 0.f) != 0.f)) {
@@ -168,55 +171,88 @@ __global__ __launch_bounds__(256) void window_fold_kernel(WindowArgs a, KeyGrid 
 // Rows on 16 bytes, whole 16-byte chunks to a head, offsets within a tile of 64 rows in 32 bits.
 static bool strides_fit(const FaxStrides& s, int unit) { return s.batch % unit == 0 && s.row % unit == 0 && s.head % unit == 0 && s.row <= (1 << 24); }
 
+// Into how many parts a stream of `tiles` tiles is cut, with `blocks` workgroups: by an estimate in us.  tile: of a tile, part_tile: of a tile
+// in a cut stream; at_once: workgroups that the chip works on side by side without slowing each other down; part_bytes: what a part writes and the joining
+// kernel reads.  6 us: the second kernel.
+struct StreamCost { double tile, part_tile, at_once; bool whole_rounds; };
+static int cut_stream(double blocks, long long tiles, const StreamCost& c, double part_bytes) {
+  int best = 1;
+  double least = tiles * c.tile;
+  for (int n = 2; n <= 64 && n <= tiles; n++) {  // (64: a lane of the joining wavefront each)
+    double rounds = blocks * n / c.at_once;
+    if (rounds < 1.0) rounds = 1.0;
+    else if (c.whole_rounds) rounds = ceil(rounds);
+    const double us = 6.0 + (double)((tiles + n - 1) / n) * c.part_tile * rounds + part_bytes * n / 2.5e6;
+    if (us < 0.97 * least) { least = us; best = n; }
+  }
+  return best;
+}
+
+// Measured, back to back in a graph, us by parts (bf16, heads on key heads x width, window):
+//   forward  512 queries over 2048 keys, 8 on 8 x 128, 2048 (32 workgroups, 34 tiles)   1: 49  4: 29  8: 27  16: 29;  16 on 4 over 8192 (64)  52  37  35  44;
+//            two of that (128) 53  47  56;  three (192) 54  2: 68;  16 on 4 x 64, 1024 (64, 18 tiles) 23  21  25;  1024 of 16 x 64, 300 (128, 7 tiles) 14.5  2: 24
+//            tokens over 4096 keys, 32 on 8 x 128: one (8 workgroups) 149  4: 54  8: 30  16: 19  32: 13  64: 12;  four 150  55  32  22  26;  sixteen 150  57  61  68
+//   dQ       4096 of 2 on 1 x 128, all (64, up to 64 tiles), of both kernels 363  2: 302  4: 272  8: 269  16: 282;  1024 of 16 x 64, 300 38  2: 43
+//   dK, dV   the same two 363  262  212  192  201;  38  45  49
 static WindowPlan window_plan(const FaxWindowDims& d) {
   WindowPlan p = {};
   p.form = FAX_ATTENTION_SCALAR;
   p.waves = 1;
-  p.row_splits = p.kv_splits = 1;
-  const int unit = d.dtype == FAX_F32 ? 4 : 8;
-  const long long heads = (long long)d.B * d.Hkv, rows = (long long)d.Sq * (d.H / d.Hkv);
+  p.fwd_splits = p.dq_splits = p.sink_splits = p.rest_splits = 1;
+  const int unit = d.dtype == FAX_F32 ? 4 : 8, group = d.H / d.Hkv;
+  const long long heads = (long long)d.B * d.Hkv, rows = (long long)d.Sq * group;
   if (d.dh % unit == 0 && d.dh <= 128 && strides_fit(d.q, unit) && strides_fit(d.kv, unit) && strides_fit(d.ctx, unit) && rows < (1 << 30)) {
     const bool f32 = d.dtype == FAX_F32;
     p.form = f32 ? FAX_ATTENTION_F32 : d.dh == 64 || d.dh == 128 ? FAX_ATTENTION_MFMA : FAX_ATTENTION_EDGE;
     p.waves = !f32 && rows > 32 ? 4 : 1;
-    const long long blocks = (rows + 32 * p.waves - 1) / (32 * p.waves) * heads;
-    // Streams are cut where there are fewer than two workgroups to a CU, into parts of at least two tiles.
-    auto cut = [](long long blocks, long long tiles) {
-      long long n = blocks < 512 ? 512 / blocks : 1;
-      if (n > tiles / 2) n = tiles / 2;
-      if (n > 64) n = 64;  // (a lane of the joining wavefront each)
-      return n > 1 ? (int)n : 1;
-    };
-    const long long seen = (long long)d.window + d.sinks + 128 < d.Sk ? d.window + d.sinks + 128 : d.Sk;  // keys that a row's workgroup meets
-    p.row_splits = cut(blocks, (seen + 63) / 64);
+    const double blocks = (double)((rows + 32 * p.waves - 1) / (32 * p.waves) * heads), row_bytes = 8.0 * d.dh * rows * heads;
+    const long long span = (rows < 32 * p.waves ? rows : 32 * p.waves) / group + 1;  // positions of a workgroup's rows
+    const long long seen = (long long)d.window + d.sinks + span < d.Sk ? d.window + d.sinks + span : d.Sk;
+    // A tile is 64 keys (queries), of fp32 a round of 32 for each of the workgroup's four wavefronts, which the matrix cores bound.
+    const bool alone = !f32 && p.waves == 1;  // a wavefront with tiles of its own: its workgroups are two to a CU
+    const int unit_keys = f32 ? 128 : 64;
+    const double w = d.dh / 128.0;
+    const StreamCost fwd = f32 ? StreamCost{1 + 3.4 * w, 1 + 3.4 * w, 256, false} : alone ? StreamCost{2.3, 2.3, 512, true} : StreamCost{1.35, 1.7, 384, false};
+    const StreamCost dq = f32 ? StreamCost{1 + 5.1 * w, 1 + 5.1 * w, 256, false} : alone ? StreamCost{3.0, 3.0, 512, true} : StreamCost{2.0, 2.0, 384, false};
+    const StreamCost dkv = f32 ? StreamCost{1 + 6.8 * w, 1 + 6.8 * w, 256, false} : StreamCost{2.0, 2.0, 400, false};
+    auto tiles = [&](long long keys) { return (keys + unit_keys - 1) / unit_keys; };
+    p.fwd_splits = cut_stream(blocks, tiles(seen), fwd, row_bytes);
+    p.dq_splits = cut_stream(blocks, tiles(seen), dq, row_bytes);
+    // Keys: those among the sinks are seen by every later query, the others by a window's length of them.
     p.kv_keys = f32 ? 32 : window_dkv_keys(d.dh);
-    const int n = (d.Sk + p.kv_keys - 1) / p.kv_keys, sinks = d.sinks < d.Sk ? d.sinks : d.Sk;
-    const long long usual = (long long)d.window + p.kv_keys + 64;  // queries that see a tile without sinks
-    p.cut_tiles = (sinks + p.kv_keys - 1) / p.kv_keys;
-    if (p.cut_tiles > 0 && 2 * p.cut_tiles <= n && d.Sq > usual) p.kv_splits = (int)(d.Sq / usual + 1 < 32 ? d.Sq / usual + 1 : 32);
-    const int all = cut(n * heads, ((d.Sq < usual ? d.Sq : usual) + 63) / 64 * (d.H / d.Hkv));
-    if (all > 1) {
-      p.cut_tiles = n;
-      if (all > p.kv_splits) p.kv_splits = all;
+    const long long n = (d.Sk + p.kv_keys - 1) / p.kv_keys, sinks = d.sinks < d.Sk ? d.sinks : d.Sk, all = tiles((long long)d.Sq * group);
+    const long long usual = (long long)d.window + p.kv_keys + 64, stream = usual < d.Sq ? tiles(usual * group) : all;
+    const double key_bytes = 16.0 * d.dh * p.kv_keys;  // of a tile
+    p.sink_tiles = (int)((sinks + p.kv_keys - 1) / p.kv_keys);
+    p.rest_splits = cut_stream((double)((n - p.sink_tiles) * heads), stream, dkv, key_bytes * (n - p.sink_tiles) * heads);
+    const long long chain = (stream + p.rest_splits - 1) / p.rest_splits;
+    if (p.sink_tiles > 0 && 2 * p.sink_tiles <= n) {  // as long as the others' parts
+      const long long parts = (all + chain - 1) / chain;
+      p.sink_splits = (int)(parts < 64 ? parts : 64);
+    } else {  // most keys are sinks: one kind of tile
+      p.sink_tiles = 0;
+      if (sinks > 0) p.rest_splits = cut_stream((double)(n * heads), all, dkv, key_bytes * n * heads);
     }
-    if (p.kv_splits == 1) p.cut_tiles = 0;
   }
   size_t o = 0;
   auto take = [&](size_t bytes) { const size_t r = o; o += (bytes + 255) / 256 * 256; return r; };
   // forward pass and backward pass take turns in the workspace
   const size_t all_rows = (size_t)d.B * d.H * d.Sq;
-  if (p.row_splits > 1) {
-    p.part_o = take(all_rows * p.row_splits * d.dh * 4);
-    p.part_ml = take(all_rows * p.row_splits * 8);
+  if (p.fwd_splits > 1) {
+    p.part_o = take(all_rows * p.fwd_splits * d.dh * 4);
+    p.part_ml = take(all_rows * p.fwd_splits * 8);
   }
   const size_t fwd = o;
   o = 0;
   p.delta = take(all_rows * 4);
-  if (p.row_splits > 1) {
-    p.part_dq = take(all_rows * p.row_splits * d.dh * 4);
-    p.part_ds = take(all_rows * p.row_splits * 4);
+  if (p.dq_splits > 1) {
+    p.part_dq = take(all_rows * p.dq_splits * d.dh * 4);
+    p.part_ds = take(all_rows * p.dq_splits * 4);
   }
-  if (p.kv_splits > 1) p.parts = take((size_t)p.kv_splits * heads * p.cut_tiles * p.kv_keys * 2 * d.dh * 4);
+  if (p.sink_splits > 1 || p.rest_splits > 1) {
+    const WindowArgs a = window_args(d);
+    p.parts = take((size_t)KeyGrid(a, p).part_rows(a) * 2 * d.dh * 4);
+  }
   p.total = o > fwd ? o : fwd;
   return p;
 }
@@ -224,8 +260,8 @@ size_t window_ws_bytes(const FaxWindowDims& d) { return window_plan(d).total; }
 void window_route(const FaxWindowDims& d, FaxWindowRoute* out) {
   const WindowPlan p = window_plan(d);
   out->form = p.form;
-  out->waves = p.waves; out->row_splits = p.row_splits; out->kv_splits = p.kv_splits;
-  out->cut_keys = p.cut_tiles * p.kv_keys;
+  out->waves = p.waves; out->fwd_splits = p.fwd_splits; out->dq_splits = p.dq_splits;
+  out->sink_splits = p.sink_splits; out->key_splits = p.rest_splits;
 }
 static bool on16(std::initializer_list<const void*> p) {
   uintptr_t all = 0;
@@ -261,13 +297,13 @@ int window_fwd(const FaxWindowDims& d, const void* q, const void* k, const void*
   } else {
     float* part_o = (float*)(w + p.part_o);
     float2* part_ml = (float2*)(w + p.part_ml);
-    if (p.form == FAX_ATTENTION_F32) FAX_TRY(window_fwd_f32(a, p.row_splits, part_o, part_ml, s));
-    else FAX_TRY(window_fwd_mfma(a, p.waves, p.row_splits, part_o, part_ml, s));
-    if (p.row_splits > 1) {
+    if (p.form == FAX_ATTENTION_F32) FAX_TRY(window_fwd_f32(a, p.fwd_splits, part_o, part_ml, s));
+    else FAX_TRY(window_fwd_mfma(a, p.waves, p.fwd_splits, part_o, part_ml, s));
+    if (p.fwd_splits > 1) {
       const float log2e = 1.4426950408889634f;
       const dim3 grid((unsigned)(((long long)a.B * a.H * a.Sq + 3) / 4));
-      if (d.dtype == FAX_F32) hipLaunchKernelGGL(window_join_kernel<float>, grid, dim3(256), 0, s, a, p.row_splits, part_o, part_ml, log2e, 1.f);
-      else hipLaunchKernelGGL(window_join_kernel<bf16_t>, grid, dim3(256), 0, s, a, p.row_splits, part_o, part_ml, a.scale * log2e, a.scale);
+      if (d.dtype == FAX_F32) hipLaunchKernelGGL(window_join_kernel<float>, grid, dim3(256), 0, s, a, p.fwd_splits, part_o, part_ml, log2e, 1.f);
+      else hipLaunchKernelGGL(window_join_kernel<bf16_t>, grid, dim3(256), 0, s, a, p.fwd_splits, part_o, part_ml, a.scale * log2e, a.scale);
     }
   }
   FAX_LAUNCH_CHECK("window_attention_fwd");
@@ -291,20 +327,19 @@ int window_bwd(const FaxWindowDims& d, const void* q, const void* k, const void*
     const unsigned row_blocks = (unsigned)(((long long)a.B * a.H * a.Sq + 3) / 4);
     if (p.form == FAX_ATTENTION_F32) {
       FAX_TRY(rows_launch<3>(a, d.dtype, s));
-      FAX_TRY(window_bwd_f32(a, p.row_splits, part_dq, p.cut_tiles, p.kv_splits, parts, s));
-      if (p.row_splits > 1) hipLaunchKernelGGL(window_fold_dq_kernel<float>, dim3(row_blocks), dim3(256), 0, s, a, p.row_splits, part_dq, (const float*)nullptr);
+      FAX_TRY(window_bwd_f32(a, p, part_dq, parts, s));
+      if (p.dq_splits > 1) hipLaunchKernelGGL(window_fold_dq_kernel<float>, dim3(row_blocks), dim3(256), 0, s, a, p.dq_splits, part_dq, (const float*)nullptr);
     } else {
       // dQ first: it also leaves delta, which dK and dV need
-      FAX_TRY(window_dq_mfma(a, p.waves, p.row_splits, part_dq, part_ds, s));
-      if (p.row_splits > 1) hipLaunchKernelGGL(window_fold_dq_kernel<bf16_t>, dim3(row_blocks), dim3(256), 0, s, a, p.row_splits, part_dq, part_ds);
-      FAX_TRY(window_dkv_mfma(a, p.cut_tiles, p.kv_splits, parts, s));
+      FAX_TRY(window_dq_mfma(a, p.waves, p.dq_splits, part_dq, part_ds, s));
+      if (p.dq_splits > 1) hipLaunchKernelGGL(window_fold_dq_kernel<bf16_t>, dim3(row_blocks), dim3(256), 0, s, a, p.dq_splits, part_dq, part_ds);
+      FAX_TRY(window_dkv_mfma(a, p, parts, s));
     }
-    if (p.kv_splits > 1) {
-      const KeyGrid kg(a, p.kv_keys, p.cut_tiles, p.kv_splits);
-      const long long keys = (long long)(p.cut_tiles * p.kv_keys < a.Sk ? p.cut_tiles * p.kv_keys : a.Sk) * a.B * a.Hkv;
-      const dim3 grid((unsigned)((keys + 3) / 4));
-      if (d.dtype == FAX_F32) hipLaunchKernelGGL(window_fold_kernel<float>, grid, dim3(256), 0, s, a, kg, p.kv_keys, parts);
-      else hipLaunchKernelGGL(window_fold_kernel<bf16_t>, grid, dim3(256), 0, s, a, kg, p.kv_keys, parts);
+    if (p.sink_splits > 1 || p.rest_splits > 1) {
+      const KeyGrid kg(a, p);
+      const dim3 grid((unsigned)(((long long)kg.fold_keys(a) * a.B * a.Hkv + 3) / 4));
+      if (d.dtype == FAX_F32) hipLaunchKernelGGL(window_fold_kernel<float>, grid, dim3(256), 0, s, a, kg, parts);
+      else hipLaunchKernelGGL(window_fold_kernel<bf16_t>, grid, dim3(256), 0, s, a, kg, parts);
     }
   }
   FAX_LAUNCH_CHECK("window_attention_bwd");

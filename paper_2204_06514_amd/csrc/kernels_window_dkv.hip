@@ -76,8 +76,8 @@ __global__ __launch_bounds__(64 * WPG, 2) void window_dkv_mfma_kernel(WindowArgs
   if (EDGE) clear_lds(smem, 2 * Stream::STAGE);
   const int j0w = it_.tile * RT + wave * 32, jk = j0w + (lane & 31);
   Stream qs(a, b, hk, QueryRange(a, sq, it_.tile * RT, min((it_.tile + 1) * RT, a.Sk)), wave, lds_addr(smem), nch);
-  const int u0 = it_.split < 0 ? 0 : (int)((long long)qs.n * it_.split / kg.splits);
-  const int u1 = it_.split < 0 ? qs.n : (int)((long long)qs.n * (it_.split + 1) / kg.splits);
+  const int u0 = (int)((long long)qs.n * it_.split / it_.splits);
+  const int u1 = (int)((long long)qs.n * (it_.split + 1) / it_.splits);
 
   bf16x8 kf[KS], vf[KS];
   const bool key_ok = jk < sq.k_len;
@@ -197,8 +197,8 @@ __global__ __launch_bounds__(64 * WPG, 2) void window_dkv_mfma_kernel(WindowArgs
     }
   }
 
-  if (it_.split >= 0) {
-    float* o = part_row(a, kg, parts, it_.split, it_.bh, kg.cut_tiles * RT, jk);
+  if (it_.splits > 1) {
+    float* o = parts + kg.part(a, it_.split, it_.bh, jk) * 2 * a.dh;
 #pragma unroll
     for (int dt = 0; dt < DT; dt++)
 #pragma unroll
@@ -247,8 +247,8 @@ __global__ __launch_bounds__(64 * WPG, 2) void window_dkv16_mfma_kernel(WindowAr
   if (EDGE) clear_lds(smem, 2 * Stream::STAGE);
   const int j0w = it_.tile * RT + wave * 16, jk = j0w + (lane & 15);
   Stream qs(a, b, hk, QueryRange(a, sq, it_.tile * RT, min((it_.tile + 1) * RT, a.Sk)), wave, lds_addr(smem), nch);
-  const int u0 = it_.split < 0 ? 0 : (int)((long long)qs.n * it_.split / kg.splits);
-  const int u1 = it_.split < 0 ? qs.n : (int)((long long)qs.n * (it_.split + 1) / kg.splits);
+  const int u0 = (int)((long long)qs.n * it_.split / it_.splits);
+  const int u1 = (int)((long long)qs.n * (it_.split + 1) / it_.splits);
 
   bf16x8 kf[KS], vf[KS];
   const bool key_ok = jk < sq.k_len;
@@ -369,8 +369,8 @@ __global__ __launch_bounds__(64 * WPG, 2) void window_dkv16_mfma_kernel(WindowAr
     }
   }
 
-  if (it_.split >= 0) {
-    float* o = part_row(a, kg, parts, it_.split, it_.bh, kg.cut_tiles * RT, jk);
+  if (it_.splits > 1) {
+    float* o = parts + kg.part(a, it_.split, it_.bh, jk) * 2 * a.dh;
 #pragma unroll
     for (int dt = 0; dt < DT; dt++) {
       const int d = dt * 16 + gq * 4;
@@ -408,9 +408,9 @@ __global__ __launch_bounds__(64 * WPG, 2) void window_dkv16_mfma_kernel(WindowAr
 
 int window_dkv_keys(int dh) { return (dh <= 64 ? 32 : 16) * WPG; }
 
-int window_dkv_mfma(const WindowArgs& a, int cut_tiles, int splits, float* parts, hipStream_t s) {
-  const KeyGrid kg(a, window_dkv_keys(a.dh), cut_tiles, splits);
-  const unsigned grid = kg.blocks(a.B * a.Hkv);
+int window_dkv_mfma(const WindowArgs& a, const WindowPlan& p, float* parts, hipStream_t s) {
+  const KeyGrid kg(a, p);
+  const unsigned grid = kg.blocks(a);
   auto launch = [&](auto kern, size_t row) -> int {
     const size_t lds = 2 * (2 * (size_t)TR * row * 2 + 4 * 256);
     FAX_HIP(hipFuncSetAttribute(reinterpret_cast<const void*>(kern), hipFuncAttributeMaxDynamicSharedMemorySize, (int)lds));

@@ -215,7 +215,7 @@ __global__ __launch_bounds__(256, DH > 64 ? 1 : 2) void window_bwd_f32_kernel(Wi
   zero<DH>(dv);
   const QueryRange all(a, sq, k0, k0 + keys), mine(a, sq, min(k0 + l31, a.Sk - 1), min(k0 + l31, a.Sk - 1) + 1);
   const int i_first = all.i0 / F32_TILE * F32_TILE, per_head = all.i0 < all.i1 ? (all.i1 - i_first + F32_TILE - 1) / F32_TILE : 0, n = per_head * a.group;
-  const int u0 = it.split < 0 ? 0 : (int)((long long)n * it.split / kg.splits), u1 = it.split < 0 ? n : (int)((long long)n * (it.split + 1) / kg.splits);
+  const int u0 = (int)((long long)n * it.split / it.splits), u1 = (int)((long long)n * (it.split + 1) / it.splits);
   for (int u = u0 + wave; u < u1; u += 4) {
     const int q0 = i_first + u % per_head * F32_TILE, head = hk * a.group + u / per_head;
     const HeadTile<DH, EXACT> Q{strided_row((const float*)a.q, a.sq, b, 0, head), (int)a.sq.row, a.Sq, dh};
@@ -255,8 +255,8 @@ __global__ __launch_bounds__(256, DH > 64 ? 1 : 2) void window_bwd_f32_kernel(Wi
   float* vo = strided_row((float*)a.dv, a.skv, b, k0, hk);
   int ld = (int)a.skv.row, rows = keys;
   float mul = a.scale;
-  if (it.split >= 0) {
-    ko = part_row(a, kg, parts, it.split, it.bh, kg.cut_tiles * F32_TILE, k0);
+  if (it.splits > 1) {
+    ko = parts + kg.part(a, it.split, it.bh, k0) * 2 * dh;
     vo = ko + dh;
     ld = 2 * dh;
     rows = F32_TILE;
@@ -303,17 +303,17 @@ int window_fwd_f32(const WindowArgs& a, int splits, float* part_o, void* part_ml
   });
 }
 
-int window_bwd_f32(const WindowArgs& a, int dq_splits, float* part_dq, int cut_tiles, int splits, float* parts, hipStream_t s) {
+int window_bwd_f32(const WindowArgs& a, const WindowPlan& p, float* part_dq, float* parts, hipStream_t s) {
   const int n_tiles = (int)(((long long)a.Sq * a.group + 31) / 32), heads = a.B * a.Hkv;
-  const long long items = (long long)n_tiles * heads * dq_splits;
-  const KeyGrid kg(a, F32_TILE, cut_tiles, splits);
-  const unsigned kv_blocks = kg.blocks(heads);
+  const long long items = (long long)n_tiles * heads * p.dq_splits;
+  const KeyGrid kg(a, p);
+  const unsigned kv_blocks = kg.blocks(a);
   return by_width(a.dh, [&](auto dw, auto exact) -> int {
     constexpr int DH = decltype(dw)::value;
     auto kern = window_bwd_f32_kernel<DH, decltype(exact)::value>;
     constexpr int lds = 4 * slot_floats<DH>() * (int)sizeof(float);
     FAX_HIP(hipFuncSetAttribute(reinterpret_cast<const void*>(kern), hipFuncAttributeMaxDynamicSharedMemorySize, lds));
-    hipLaunchKernelGGL(kern, dim3(kv_blocks + xcd_grid(items)), dim3(256), lds, s, a, kg, (int)kv_blocks, n_tiles, (int)items, dq_splits, part_dq, parts);
+    hipLaunchKernelGGL(kern, dim3(kv_blocks + xcd_grid(items)), dim3(256), lds, s, a, kg, (int)kv_blocks, n_tiles, (int)items, p.dq_splits, part_dq, parts);
     return FAX_OK;
   });
 }

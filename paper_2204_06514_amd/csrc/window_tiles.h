@@ -32,42 +32,50 @@ __device__ __forceinline__ bool sees_any(const WindowArgs& a, int k_len, int p0,
 }
 
 // dK and dV.  A workgroup has a tile of keys of one key head and streams the tiles of queries of all its query heads that see some of
-// them, head by head.  The streams of the first `cut_tiles` tiles are cut into `splits` parts, workgroups of their own that leave sums for
-// window_fold_kernel: those of the sinks, which every later query sees and not a window's length of them, or of all, where tiles are few.
-// They are the first workgroups of the launch; the other tiles follow.
+// them, head by head.  A stream may be cut into parts, workgroups of their own that leave sums for window_fold_kernel: `sink_splits` of the tiles with
+// sinks, which every later query sees, `rest_splits` of the others.  The sinks' workgroups are the first of the launch.
 struct KeyGrid {
-  int n_tiles, cut_tiles, splits, cut_blocks;  // key tiles of a head; how many of them are cut, into how many parts; workgroups of those
-  KeyGrid(const WindowArgs& a, int keys, int cut_tiles_, int splits_) {
+  int keys, n_tiles, sink_tiles, sink_splits, rest_splits, sink_blocks;
+  KeyGrid(const WindowArgs& a, const WindowPlan& p) {
+    keys = p.kv_keys;
     n_tiles = (a.Sk + keys - 1) / keys;
-    cut_tiles = splits_ > 1 ? cut_tiles_ : 0;
-    splits = splits_;
-    cut_blocks = (int)xcd_grid((long long)cut_tiles * a.B * a.Hkv * splits);
+    sink_tiles = p.sink_tiles;
+    sink_splits = p.sink_splits;
+    rest_splits = p.rest_splits;
+    sink_blocks = (int)xcd_grid((long long)sink_tiles * a.B * a.Hkv * sink_splits);
   }
-  unsigned blocks(int heads) const { return cut_blocks + xcd_grid((long long)(n_tiles - cut_tiles) * heads); }
+  unsigned blocks(const WindowArgs& a) const { return sink_blocks + xcd_grid((long long)(n_tiles - sink_tiles) * a.B * a.Hkv * rest_splits); }
+  // Rows of scratch (dK and dV of a key in a part): the sinks' parts [part, key head, key], then the others'.
+  __host__ __device__ __forceinline__ long long sink_rows(const WindowArgs& a) const { return sink_splits > 1 ? (long long)sink_splits * a.B * a.Hkv * sink_tiles * keys : 0; }
+  long long part_rows(const WindowArgs& a) const {
+    return sink_rows(a) + (rest_splits > 1 ? (long long)rest_splits * a.B * a.Hkv * (n_tiles - sink_tiles) * keys : 0);
+  }
+  __device__ __forceinline__ long long part(const WindowArgs& a, int split, int bh, int j) const {
+    const int first = sink_tiles * keys;
+    if (j < first) return ((long long)split * a.B * a.Hkv + bh) * first + j;
+    return sink_rows(a) + ((long long)split * a.B * a.Hkv + bh) * ((n_tiles - sink_tiles) * keys) + j - first;
+  }
+  // the keys whose parts are added up: [fold_from, fold_from + fold_keys)
+  __host__ __device__ __forceinline__ int fold_from() const { return sink_splits > 1 ? 0 : sink_tiles * keys; }
+  __host__ __device__ __forceinline__ int fold_keys(const WindowArgs& a) const {
+    const int end = rest_splits > 1 ? a.Sk : sink_tiles * keys;
+    return (end < a.Sk ? end : a.Sk) - fold_from();
+  }
 };
 struct KeyItem {
-  int bh, tile, split;  // split < 0: whole
+  int bh, tile, split, splits;  // splits 1: whole
   bool ok;
   __device__ __forceinline__ KeyItem(const KeyGrid& k, int heads, int block, int grid) {
-    if (block < k.cut_blocks) {
-      split = block % k.splits;
-      const int r = block / k.splits;
-      tile = r % max(k.cut_tiles, 1);
-      bh = r / max(k.cut_tiles, 1);
-      ok = bh < heads;
-    } else {
-      const int rest = k.n_tiles - k.cut_tiles, i = xcd_item(block - k.cut_blocks, grid - k.cut_blocks);
-      split = -1;
-      ok = i < rest * heads;
-      tile = k.cut_tiles + i % max(rest, 1);
-      bh = i / max(rest, 1);
-    }
+    const bool sinks = block < k.sink_blocks;
+    const int tiles = max(sinks ? k.sink_tiles : k.n_tiles - k.sink_tiles, 1);
+    int i = sinks ? block : xcd_item(block - k.sink_blocks, grid - k.sink_blocks);
+    splits = sinks ? k.sink_splits : k.rest_splits;
+    split = i % splits;
+    i /= splits;
+    bh = i / tiles;
+    tile = (sinks ? 0 : k.sink_tiles) + i % tiles;
+    ok = bh < heads && tile < k.n_tiles;
   }
 };
-
-// A part's row of scratch: [part, head, key of the cut tiles, dK | dV, feature].
-__device__ __forceinline__ float* part_row(const WindowArgs& a, const KeyGrid& k, float* parts, int split, int bh, int keys, int j) {
-  return parts + ((((long long)split * a.B * a.Hkv + bh) * keys + j) * 2) * a.dh;
-}
 
 }  // namespace fax

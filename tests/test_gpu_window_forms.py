@@ -29,21 +29,23 @@ def test_four_wavefronts(dh, H, Hkv, window, sinks):
     if Hkv == 10 and dh in (40, 104):
         pytest.skip("two widths are enough for grouped heads")
     r = route(1, S, S, H, Hkv, dh, "bf16", window, sinks)
-    assert (r.waves, r.row_splits) == (4, 1), forms(r)
+    assert (r.waves, r.fwd_splits, r.dq_splits) == (4, 1, 1) and r.sink_splits > 1 or window > 100, forms(r)
     if Hkv == 32:
-        assert (r.kv_splits > 1) == (window == 100) and r.cut_keys < S, forms(r)
+        assert r.key_splits == 1, forms(r)
     both(1, S, S, H, Hkv, dh, "bf16", window, sinks, torch.tensor([0], dtype=torch.int32), torch.tensor([S - 70], dtype=torch.int32))
 
 
 @pytest.mark.parametrize("dtype", ["bf16", "f32"])
 @pytest.mark.parametrize("dh", [24, 64, 96, 128])
-@pytest.mark.parametrize("S,H,Hkv,window,sinks", [(700, 2, 1, 10000, 0), (900, 4, 4, 200, 3), (1500, 8, 1, 64, 70), (130, 1, 1, 130, 130)])
+@pytest.mark.parametrize("S,H,Hkv,window,sinks", [(1500, 2, 1, 10000, 0), (1500, 4, 4, 1000, 3), (1500, 8, 1, 64, 70), (1500, 1, 1, 700, 1500)])
 def test_cut_streams(S, H, Hkv, window, sinks, dh, dtype):
     r = route(1, S, S, H, Hkv, dh, dtype, window, sinks)
-    if S > 130:
-        assert r.row_splits > 1 or r.kv_splits > 1, forms(r)
-    if S == 700:
-        assert r.row_splits > 1 and r.kv_splits > 1 and r.cut_keys >= S, forms(r)
+    if H == 2 or (H == 4 and dtype == "bf16"):
+        assert min(r.dq_splits, r.key_splits) > 1 and (r.fwd_splits > 1 or H == 4) and (r.sink_splits > 1) == (H == 4), forms(r)
+    if sinks == 70:
+        assert r.sink_splits > 1, forms(r)
+    if sinks == 1500:
+        assert r.sink_splits == 1 and r.key_splits > 1, forms(r)
     both(1, S, S, H, Hkv, dh, dtype, window, sinks)
 
 
@@ -51,7 +53,7 @@ def test_cut_streams(S, H, Hkv, window, sinks, dh, dtype):
 def test_sinks_alone_are_cut(dtype):
     B, S, H, window, sinks = 6, 1400, 8, 20, 5
     r = route(B, S, S, H, H, 64, dtype, window, sinks)
-    assert r.kv_splits > 1 and 0 < r.cut_keys < S, forms(r)
+    assert r.sink_splits > 1 and r.key_splits == 1, forms(r)
     both(B, S, S, H, H, 64, dtype, window, sinks)
 
 
