@@ -26,20 +26,12 @@ struct QueryStream {
 #pragma unroll
     for (int i = 0; i < NSEG; i++) in_head[i] = !EDGE || lane_in_head<DH, WAVES, SWZ16>(wave, i, nch);
   }
-  __device__ __forceinline__ int query(int u) const { return i_first + u % per_head * TR; }
-  __device__ __forceinline__ int head(int u) const { return hk * a.group + u / per_head; }
-  // Tile u into buffer `buf`: segments of Q and dO, then lse and delta (lanes 0-15 lse, 16-31 delta, the others the same again).
-  __device__ __forceinline__ void load(int u, int buf) const {
-    const int i0 = query(u), h = head(u), rows = a.Sq - i0;
+  // Tile t of head g (of the key head's) into buffer `buf`: segments of Q and dO, then lse and delta (lanes 0-15 lse, 16-31 delta, the others the
+  // same again).
+  __device__ __forceinline__ void load(int g, int t, int buf) const {
+    const int i0 = i_first + t * TR, h = hk * a.group + g, rows = a.Sq - i0;
     const unsigned st = sm + buf * STAGE;
-    const bf16_t* qt = strided_row((const bf16_t*)a.q, a.sq, b, i0, h);
-    const bf16_t* dt = strided_row((const bf16_t*)a.dctx, a.sc, b, i0, h);
-#pragma unroll
-    for (int i = 0; i < NSEG; i++)
-      if (in_head[i]) {
-        q.segment(qt, rows, st, i);
-        dout.segment(dt, rows, st + TB, i);
-      }
+    load_pair(q, dout, strided_row((const bf16_t*)a.q, a.sq, b, i0, h), strided_row((const bf16_t*)a.dctx, a.sc, b, i0, h), rows, st, st + TB, in_head);
     const long long stat = ((long long)b * a.H + h) * a.Sq + i0;
 #pragma unroll
     for (int i = 0; i < 4 / WAVES; i++) {
@@ -157,41 +149,34 @@ __global__ __launch_bounds__(64 * WPG, 2) void window_dkv_mfma_kernel(WindowArgs
   };
 
   if (u0 < u1) {
-    qs.load(u0, 0);
+    int g_at = u0 / qs.per_head, t = u0 - g_at * qs.per_head;  // head and tile of u
+    qs.load(g_at, t, 0);
     lds_dma_wait();
     __syncthreads();
     // Runs of tiles with and without masks in loops of their own, as in the forward pass.
-    auto positions = [&](int u, int& p0, int& p1) __attribute__((always_inline)) {
-      const int i0 = qs.query(u);
-      p0 = sq.pos0 + i0;
-      p1 = p0 + min(TR, a.Sq - i0) - 1;
-    };
-    auto full = [&](int u) __attribute__((always_inline)) {
-      int p0, p1;
-      positions(u, p0, p1);
-      return p1 - p0 == TR - 1 && sees_all(a, sq.k_len, p0, p1, j0w, 32);
-    };
-    auto any = [&](int u) __attribute__((always_inline)) {
-      int p0, p1;
-      positions(u, p0, p1);
-      return sees_any(a, sq.k_len, p0, p1, j0w, 32);
+    const FullRun full = FullRun::queries(a, sq, j0w, j0w + 32 - 1, qs.i_first);
+    auto any = [&](int t) __attribute__((always_inline)) {
+      const int i0 = qs.i_first + t * TR, p0 = sq.pos0 + i0;
+      return sees_any(a, sq.k_len, p0, p0 + min(TR, a.Sq - i0) - 1, j0w, 32);
     };
     auto next = [&](int u) __attribute__((always_inline)) {
-      if (u + 1 < u1) qs.load(u + 1, (u - u0 + 1) & 1);
+      const bool same = t + 1 < qs.per_head;
+      if (u + 1 < u1) qs.load(same ? g_at : g_at + 1, same ? t + 1 : 0, (u - u0 + 1) & 1);
     };
     auto done = [&]() __attribute__((always_inline)) {
       lds_dma_wait();
       __syncthreads();
+      if (++t == qs.per_head) { t = 0; g_at++; }
     };
     for (int u = u0; u < u1;) {
-      for (; u < u1 && !full(u); u++) {
+      for (; u < u1 && !full.has(t); u++) {
         next(u);
-        if (any(u)) tile(T_{}, qs.query(u), (u - u0) & 1);
+        if (any(t)) tile(T_{}, qs.i_first + t * TR, (u - u0) & 1);
         done();
       }
-      for (; u < u1 && full(u); u++) {
+      for (; u < u1 && full.has(t); u++) {
         next(u);
-        tile(F_{}, qs.query(u), (u - u0) & 1);
+        tile(F_{}, qs.i_first + t * TR, (u - u0) & 1);
         done();
       }
     }
@@ -329,41 +314,34 @@ __global__ __launch_bounds__(64 * WPG, 2) void window_dkv16_mfma_kernel(WindowAr
   };
 
   if (u0 < u1) {
-    qs.load(u0, 0);
+    int g_at = u0 / qs.per_head, t = u0 - g_at * qs.per_head;  // head and tile of u
+    qs.load(g_at, t, 0);
     lds_dma_wait();
     __syncthreads();
     // Runs of tiles with and without masks in loops of their own, as in the forward pass.
-    auto positions = [&](int u, int& p0, int& p1) __attribute__((always_inline)) {
-      const int i0 = qs.query(u);
-      p0 = sq.pos0 + i0;
-      p1 = p0 + min(TR, a.Sq - i0) - 1;
-    };
-    auto full = [&](int u) __attribute__((always_inline)) {
-      int p0, p1;
-      positions(u, p0, p1);
-      return p1 - p0 == TR - 1 && sees_all(a, sq.k_len, p0, p1, j0w, 16);
-    };
-    auto any = [&](int u) __attribute__((always_inline)) {
-      int p0, p1;
-      positions(u, p0, p1);
-      return sees_any(a, sq.k_len, p0, p1, j0w, 16);
+    const FullRun full = FullRun::queries(a, sq, j0w, j0w + 16 - 1, qs.i_first);
+    auto any = [&](int t) __attribute__((always_inline)) {
+      const int i0 = qs.i_first + t * TR, p0 = sq.pos0 + i0;
+      return sees_any(a, sq.k_len, p0, p0 + min(TR, a.Sq - i0) - 1, j0w, 16);
     };
     auto next = [&](int u) __attribute__((always_inline)) {
-      if (u + 1 < u1) qs.load(u + 1, (u - u0 + 1) & 1);
+      const bool same = t + 1 < qs.per_head;
+      if (u + 1 < u1) qs.load(same ? g_at : g_at + 1, same ? t + 1 : 0, (u - u0 + 1) & 1);
     };
     auto done = [&]() __attribute__((always_inline)) {
       lds_dma_wait();
       __syncthreads();
+      if (++t == qs.per_head) { t = 0; g_at++; }
     };
     for (int u = u0; u < u1;) {
-      for (; u < u1 && !full(u); u++) {
+      for (; u < u1 && !full.has(t); u++) {
         next(u);
-        if (any(u)) tile(T_{}, qs.query(u), (u - u0) & 1);
+        if (any(t)) tile(T_{}, qs.i_first + t * TR, (u - u0) & 1);
         done();
       }
-      for (; u < u1 && full(u); u++) {
+      for (; u < u1 && full.has(t); u++) {
         next(u);
-        tile(F_{}, qs.query(u), (u - u0) & 1);
+        tile(F_{}, qs.i_first + t * TR, (u - u0) & 1);
         done();
       }
     }

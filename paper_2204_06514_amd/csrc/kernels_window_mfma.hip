@@ -56,12 +56,7 @@ __global__ __launch_bounds__(64 * WPG, 2) void window_fwd_mfma_kernel(WindowArgs
   for (int i = 0; i < NSEG; i++) in_head[i] = !EDGE || lane_in_head<DH, WPG, false>(wave, i, nch);
   auto load = [&](int j0, int buf) __attribute__((always_inline)) {
     const long long at = (long long)j0 * a.skv.row;
-#pragma unroll
-    for (int i = 0; i < NSEG; i++)
-      if (in_head[i]) {
-        loads.segment(kb + at, sq.k_len - j0, sm + buf * 2 * TB, i);
-        loads.segment(vb + at, sq.k_len - j0, sm + buf * 2 * TB + TB, i);
-      }
+    load_pair(loads, loads, kb + at, vb + at, sq.k_len - j0, sm + buf * 2 * TB, sm + buf * 2 * TB + TB, in_head);
   };
   const int p = rt.p, last = min(p, sq.k_len - 1), first = p - a.window;  // sees keys in (first, last] and the sinks up to last
   auto tile = [&](auto mask_c, int j0, int buf) __attribute__((always_inline)) {
@@ -154,7 +149,7 @@ __global__ __launch_bounds__(64 * WPG, 2) void window_fwd_mfma_kernel(WindowArgs
     __syncthreads();
     // Runs of tiles that take the masks (or that no row of the wave sees) and of tiles that do not, in loops of their own: one loop over both kinds
     // keeps the accumulators in two places, which does not fit the registers.
-    auto full = [&](int u) { return sees_all(a, sq.k_len, rt.wp0, rt.wp1, kt.key(u), TR); };
+    const FullRun full = FullRun::keys(a, sq.k_len, rt.wp0, rt.wp1, kt);
     auto next = [&](int u) __attribute__((always_inline)) {
       if (u + 1 < u1) load(kt.key(u + 1), (u - u0 + 1) & 1);
     };
@@ -163,12 +158,12 @@ __global__ __launch_bounds__(64 * WPG, 2) void window_fwd_mfma_kernel(WindowArgs
       __syncthreads();
     };
     for (int u = u0; u < u1;) {
-      for (; u < u1 && !full(u); u++) {
+      for (; u < u1 && !full.has(u); u++) {
         next(u);
         if (sees_any(a, sq.k_len, rt.wp0, rt.wp1, kt.key(u), TR)) tile(T_{}, kt.key(u), (u - u0) & 1);
         done();
       }
-      for (; u < u1 && full(u); u++) {
+      for (; u < u1 && full.has(u); u++) {
         next(u);
         tile(F_{}, kt.key(u), (u - u0) & 1);
         done();
@@ -268,12 +263,7 @@ __global__ __launch_bounds__(64 * WPG, 2) void window_dq_mfma_kernel(WindowArgs 
   for (int i = 0; i < NSEG; i++) in_head[i] = !EDGE || lane_in_head<DH, WPG, false>(wave, i, nch);
   auto load = [&](int j0, int buf) __attribute__((always_inline)) {
     const long long at = (long long)j0 * a.skv.row;
-#pragma unroll
-    for (int i = 0; i < NSEG; i++)
-      if (in_head[i]) {
-        loads.segment(kb + at, sq.k_len - j0, sm + buf * 2 * TB, i);
-        loads.segment(vb + at, sq.k_len - j0, sm + buf * 2 * TB + TB, i);
-      }
+    load_pair(loads, loads, kb + at, vb + at, sq.k_len - j0, sm + buf * 2 * TB, sm + buf * 2 * TB + TB, in_head);
   };
   const f32x16 zero = {0.f, 0.f, 0.f, 0.f, 0.f, 0.f, 0.f, 0.f, 0.f, 0.f, 0.f, 0.f, 0.f, 0.f, 0.f, 0.f};
   const int p = rt.p, last = min(p, sq.k_len - 1), first = p - a.window;
@@ -333,7 +323,7 @@ __global__ __launch_bounds__(64 * WPG, 2) void window_dq_mfma_kernel(WindowArgs 
     __syncthreads();
     // Runs of tiles that take the masks (or that no row of the wave sees) and of tiles that do not, in loops of their own: one loop over both kinds
     // keeps the accumulators in two places, which does not fit the registers.
-    auto full = [&](int u) { return sees_all(a, sq.k_len, rt.wp0, rt.wp1, kt.key(u), TR); };
+    const FullRun full = FullRun::keys(a, sq.k_len, rt.wp0, rt.wp1, kt);
     auto next = [&](int u) __attribute__((always_inline)) {
       if (u + 1 < u1) load(kt.key(u + 1), (u - u0 + 1) & 1);
     };
@@ -342,12 +332,12 @@ __global__ __launch_bounds__(64 * WPG, 2) void window_dq_mfma_kernel(WindowArgs 
       __syncthreads();
     };
     for (int u = u0; u < u1;) {
-      for (; u < u1 && !full(u); u++) {
+      for (; u < u1 && !full.has(u); u++) {
         next(u);
         if (sees_any(a, sq.k_len, rt.wp0, rt.wp1, kt.key(u), TR)) tile(T_{}, kt.key(u), (u - u0) & 1);
         done();
       }
-      for (; u < u1 && full(u); u++) {
+      for (; u < u1 && full.has(u); u++) {
         next(u);
         tile(F_{}, kt.key(u), (u - u0) & 1);
         done();

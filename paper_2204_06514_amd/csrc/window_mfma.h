@@ -20,11 +20,12 @@ __device__ __forceinline__ const bf16_t* uniform(const bf16_t* p) {
 }
 
 // Loads of a wave's share of a 64-row tile, 1 KB segments of RPI rows.  A lane's 16 bytes of segment i lie at its row (lane / NCH, from the segment's
-// first) and at the chunk that the swizzle puts there, of which there are OFFS different ones: those offsets are kept, the segment's first
-// row goes into the uniform base.  Of a tile with fewer than 64 rows (at least one) the last row is loaded again.
+// first) and at the chunk that the swizzle puts there.  The swizzles repeat after 16 rows, so the byte offsets of OFFS segments are kept, and the others'
+// are theirs from a base further down.  Of a tile with fewer than 64 rows (at least one) the last row is loaded again; which of the two it is, is asked once
+// for all segments (a branch for each cost a third of the forward pass).
 template <int DH, int WAVES, bool SWZ16>
 struct TileLoads {
-  static constexpr int NCH = DH / 8, RPI = 64 / NCH, NSEG = DH / 8 / WAVES, OFFS = RPI == 8 ? 1 : 16 / RPI < NSEG ? 16 / RPI : NSEG;
+  static constexpr int NCH = DH / 8, RPI = 64 / NCH, NSEG = DH / 8 / WAVES, OFFS = NSEG * RPI <= 16 ? NSEG : 16 / RPI;
   unsigned off[OFFS];
   int wave, ld;
   __device__ __forceinline__ static int chunk_of(int row) {
@@ -33,21 +34,41 @@ struct TileLoads {
   __device__ __forceinline__ TileLoads(int wave_, long long ld_) {
     wave = wave_;
     ld = (int)ld_;
-    const int r = (threadIdx.x & 63) / NCH;
 #pragma unroll
-    for (int i = 0; i < OFFS; i++) off[i] = (unsigned)(r * ld) * 2u + chunk_of((wave * NSEG + i) * RPI + r) * 16u;
-  }
-  __device__ __forceinline__ void segment(const bf16_t* tile, int rows, unsigned lds_tile, int i) const {
-    const int first = (wave * NSEG + i) * RPI;
-    const unsigned dst = __builtin_amdgcn_readfirstlane(lds_tile + (wave * NSEG + i) * 1024u);
-    if (rows >= TR) {
-      lds_dma16(uniform(tile + (long long)first * ld), off[i % OFFS], dst);
-    } else {
-      const int row = first + (threadIdx.x & 63) / NCH;
-      lds_dma16(uniform(tile), (unsigned)(min(row, rows - 1) * ld) * 2u + chunk_of(row) * 16u, dst);
+    for (int i = 0; i < OFFS; i++) {
+      const int row = (wave * NSEG + i) * RPI + (threadIdx.x & 63) / NCH;
+      off[i] = (unsigned)(row * ld) * 2u + chunk_of(row) * 16u;
     }
   }
+  // segment i of a whole tile; of one with `rows` rows
+  __device__ __forceinline__ void whole(const bf16_t* tile, unsigned lds_tile, int i) const {
+    lds_dma16(uniform(tile + (long long)(i / OFFS * OFFS * RPI) * ld), off[i % OFFS], __builtin_amdgcn_readfirstlane(lds_tile + (wave * NSEG + i) * 1024u));
+  }
+  __device__ __forceinline__ void ragged(const bf16_t* tile, int rows, unsigned lds_tile, int i) const {
+    const int row = (wave * NSEG + i) * RPI + (threadIdx.x & 63) / NCH;
+    lds_dma16(uniform(tile), (unsigned)(min(row, rows - 1) * ld) * 2u + chunk_of(row) * 16u, __builtin_amdgcn_readfirstlane(lds_tile + (wave * NSEG + i) * 1024u));
+  }
 };
+// Segments of a pair of tiles (K and V; Q and dO) of `rows` rows.
+template <int NSEG, typename LoadsA, typename LoadsB>
+__device__ __forceinline__ void load_pair(const LoadsA& x, const LoadsB& y, const bf16_t* tx, const bf16_t* ty, int rows, unsigned lds_x, unsigned lds_y,
+                                          const bool (&in_head)[NSEG]) {
+  if (rows >= TR) {
+#pragma unroll
+    for (int i = 0; i < NSEG; i++)
+      if (in_head[i]) {
+        x.whole(tx, lds_x, i);
+        y.whole(ty, lds_y, i);
+      }
+  } else {
+#pragma unroll
+    for (int i = 0; i < NSEG; i++)
+      if (in_head[i]) {
+        x.ragged(tx, rows, lds_x, i);
+        y.ragged(ty, rows, lds_y, i);
+      }
+  }
+}
 // Whether this lane's chunk of segment i lies within the head (masked-edge form).
 template <int DH, int WAVES, bool SWZ16>
 __device__ __forceinline__ bool lane_in_head(int wave, int i, int chunks) {
@@ -67,6 +88,31 @@ __device__ __forceinline__ void split2(float x, float y, bf16x8& hi, bf16x8& lo,
   lo[2 * n] = (__bf16)(x - __uint_as_float(a & 0xffff0000u));
   lo[2 * n + 1] = (__bf16)(y - __uint_as_float(b & 0xffff0000u));
 }
+
+// Which tiles of a stream need no masks: a run of them.
+struct FullRun {
+  int first;
+  unsigned count;
+  __device__ __forceinline__ bool has(int u) const { return (unsigned)(u - first) < count; }
+  // Keys for rows at p0 .. p1 (by position; tiles of sinks that the window does not reach take the masks even where all of them are seen).
+  __device__ __forceinline__ static FullRun keys(const WindowArgs& a, int k_len, int p0, int p1, const KeyTiles<TR>& kt) {
+    const int from = max(0, p1 - a.window + 1), to = min(p0 + 1, k_len);  // every row sees [from, to)
+    const int t0 = (from + TR - 1) / TR, t1 = to / TR;
+    FullRun r;
+    r.first = t0 >= kt.sink_tiles ? t0 - kt.skip : t0;
+    r.count = (unsigned)max(0, t1 - t0);
+    return r;
+  }
+  // Queries, counted in tiles from i_first, that see all of the keys j0 .. j1.
+  __device__ __forceinline__ static FullRun queries(const WindowArgs& a, const WindowSeq& s, int j0, int j1, int i_first) {
+    const long long from = max(0, j1 - s.pos0), to = j1 < a.sinks ? a.Sq : min((long long)a.Sq, (long long)j0 + a.window - s.pos0);  // [from, to)
+    const int t0 = (int)((max((long long)0, from - i_first) + TR - 1) / TR), t1 = (int)((to - i_first) / TR);
+    FullRun r;
+    r.first = t0;
+    r.count = j1 < s.k_len && to > i_first ? (unsigned)max(0, t1 - t0) : 0u;
+    return r;
+  }
+};
 
 // The rows that a workgroup of the forward pass or of dQ has, and what it streams for them.
 template <int WPG>
