@@ -94,7 +94,6 @@ __global__ __launch_bounds__(64 * WPG, 2) void window_dkv_mfma_kernel(WindowArgs
   auto tile = [&](auto mask_c, int i0, int buf) __attribute__((always_inline)) {
     constexpr bool MASK = decltype(mask_c)::value;
     int lane_t = lane;
-    settle(lane_t);  // fragment addresses are formed tile by tile: kept from tile to tile they are some thirty registers
     const char* st = smem + buf * Stream::STAGE;
     auto row_frag = [&](int it, int i) { return frag_rows<DH>(i % 2 ? st + TB : st, it * 32, i / 2, lane_t); };
     auto col_frag = [&](int it, int i) { return frag_cols<DH>(i % 2 ? st : st + TB, ((i / 2) % DT) * 32, it * 32 + (i / (2 * DT)) * 16, lane_t); };

@@ -62,7 +62,7 @@ __global__ __launch_bounds__(64 * WPG, 2) void window_fwd_mfma_kernel(WindowArgs
   auto tile = [&](auto mask_c, int j0, int buf) __attribute__((always_inline)) {
     constexpr bool MASK = decltype(mask_c)::value;
     int lane_t = lane;
-    settle(lane_t);  // fragment addresses are formed tile by tile: kept from tile to tile they are some thirty registers
+    if (DW > 64) settle(lane_t);  // fragment addresses are formed tile by tile: kept from tile to tile they are some thirty registers
     const char* kt_ = smem + buf * 2 * TB;
     const char* vt_ = kt_ + TB;
     auto row_frag = [&](int i) { return frag_rows<DH>(kt_, (i % 2) * 32, i / 2, lane_t); };
@@ -270,7 +270,7 @@ __global__ __launch_bounds__(64 * WPG, 2) void window_dq_mfma_kernel(WindowArgs 
   auto tile = [&](auto mask_c, int j0, int buf) __attribute__((always_inline)) {
     constexpr bool MASK = decltype(mask_c)::value;
     int lane_t = lane;
-    settle(lane_t);  // fragment addresses are formed tile by tile: kept from tile to tile they are some thirty registers
+    if (DW > 64) settle(lane_t);  // fragment addresses are formed tile by tile: kept from tile to tile they are some thirty registers
     const char* kt_ = smem + buf * 2 * TB;
     const char* vt_ = kt_ + TB;
     auto row_frag = [&](int jt, int i) { return frag_rows<DH>((i & 1) ? vt_ : kt_, jt * 32, i / 2, lane_t); };
