@@ -311,28 +311,42 @@ struct Piece {
       for (int e = 0; e < E; e++) x[s][e] = 0.f;
     }
   }
+  template <typename T>
+  using Vec = std::conditional_t<E == 1, T, std::conditional_t<sizeof(T) == 4, float4, uint2>>;
+  template <int R, typename T>
+  __device__ __forceinline__ void load(Vec<T> (&v)[R][STEPS], const T* const (&row)[R], int D) const {
+#pragma unroll
+    for (int r = 0; r < R; r++)
+#pragma unroll
+      for (int s = 0; s < STEPS; s++) v[r][s] = *reinterpret_cast<const Vec<T>*>(row[r] + min(at[s], D - E));
+  }
+  template <typename T>
+  __device__ __forceinline__ void add(const Vec<T> (&v)[STEPS]) {
+#pragma unroll
+    for (int s = 0; s < STEPS; s++) {
+      if constexpr (E == 1) {
+        x[s][0] += to_f(v[s]);
+      } else if constexpr (sizeof(T) == 4) {
+        x[s][0] += v[s].x; x[s][1] += v[s].y; x[s][2] += v[s].z; x[s][3] += v[s].w;
+      } else {
+        x[s][0] += __uint_as_float(v[s].x << 16); x[s][1] += __uint_as_float(v[s].x & 0xffff0000u);
+        x[s][2] += __uint_as_float(v[s].y << 16); x[s][3] += __uint_as_float(v[s].y & 0xffff0000u);
+      }
+    }
+  }
   // += R rows, in order
   template <int R, typename T>
-  __device__ __forceinline__ void add(const T* const (&row)[R], int D) {
-    typedef std::conditional_t<E == 1, T, std::conditional_t<sizeof(T) == 4, float4, uint2>> Vec;
-    Vec v[R][STEPS];
+  __device__ __forceinline__ void add_rows(const T* const (&row)[R], int D) {
+    Vec<T> v[R][STEPS];
+    load(v, row, D);
 #pragma unroll
-    for (int r = 0; r < R; r++)
+    for (int r = 0; r < R; r++) add<T>(v[r]);
+  }
+  __device__ __forceinline__ void clear() {
 #pragma unroll
-      for (int s = 0; s < STEPS; s++) v[r][s] = *reinterpret_cast<const Vec*>(row[r] + min(at[s], D - E));
+    for (int s = 0; s < STEPS; s++)
 #pragma unroll
-    for (int r = 0; r < R; r++)
-#pragma unroll
-      for (int s = 0; s < STEPS; s++) {
-        if constexpr (E == 1) {
-          x[s][0] += to_f(v[r][s]);
-        } else if constexpr (sizeof(T) == 4) {
-          x[s][0] += v[r][s].x; x[s][1] += v[r][s].y; x[s][2] += v[r][s].z; x[s][3] += v[r][s].w;
-        } else {
-          x[s][0] += __uint_as_float(v[r][s].x << 16); x[s][1] += __uint_as_float(v[r][s].x & 0xffff0000u);
-          x[s][2] += __uint_as_float(v[r][s].y << 16); x[s][3] += __uint_as_float(v[r][s].y & 0xffff0000u);
-        }
-      }
+      for (int e = 0; e < E; e++) x[s][e] = 0.f;
   }
   // scale, add to what is there where asked, store
   __device__ __forceinline__ void store(float* __restrict__ row, int D, float scale, bool accumulate) const {
@@ -353,23 +367,27 @@ struct Piece {
   }
 };
 
-// acc += the rows of positions pos[k0 .. k1): 64 positions loaded at a time and handed around, four rows in flight.
+// acc += the rows of the positions in lanes from .. from + n - 1 of `mine`, four in flight.
+template <typename T, int E, int STEPS>
+__device__ __forceinline__ void add_lanes(Piece<E, STEPS>& acc, const T* __restrict__ dout, int D, int mine, int from, int n) {
+  auto row = [&](int i) { return dout + (size_t)(unsigned)__builtin_amdgcn_readlane(mine, from + i) * D; };
+  int i = 0;
+  for (; i + 4 <= n; i += 4) {
+    const T* const r[4] = {row(i), row(i + 1), row(i + 2), row(i + 3)};
+    acc.add_rows(r, D);
+  }
+  for (; i < n; i++) {
+    const T* const r[1] = {row(i)};
+    acc.add_rows(r, D);
+  }
+}
+// acc += the rows of positions pos[k0 .. k1)
 template <typename T, int E, int STEPS>
 __device__ __forceinline__ void add_positions(Piece<E, STEPS>& acc, const T* __restrict__ dout, int D, const uint32_t* __restrict__ pos, int k0, int k1) {
   const int lane = threadIdx.x & 63;
   for (int k = k0; k < k1; k += 64) {
     const int n = min(64, k1 - k);
-    const int mine = (int)(lane < n ? pos[k + lane] : 0u);
-    auto row = [&](int i) { return dout + (size_t)(unsigned)__builtin_amdgcn_readlane(mine, i) * D; };
-    int i = 0;
-    for (; i + 4 <= n; i += 4) {
-      const T* const r[4] = {row(i), row(i + 1), row(i + 2), row(i + 3)};
-      acc.add(r, D);
-    }
-    for (; i < n; i++) {
-      const T* const r[1] = {row(i)};
-      acc.add(r, D);
-    }
+    add_lanes(acc, dout, D, (int)(lane < n ? pos[k + lane] : 0u), 0, n);
   }
 }
 
@@ -429,11 +447,11 @@ __device__ __forceinline__ void long_row(int N, int D, int c, const uint32_t* __
     auto row = [&](int i) { return sums + (size_t)i * D; };
     for (; k + 4 <= end; k += 4) {
       const float* const r[4] = {row(k), row(k + 1), row(k + 2), row(k + 3)};
-      acc.add(r, D);
+      acc.add_rows(r, D);
     }
     for (; k < end; k++) {
       const float* const r[1] = {row(k)};
-      acc.add(r, D);
+      acc.add_rows(r, D);
     }
     if (wave == 3) add_positions(acc, dout, D, pos, c1 * CHUNK, hi);
     __syncthreads();
@@ -487,17 +505,57 @@ __global__ __launch_bounds__(256) void embedding_rows_kernel(int N, int V, int D
     v = key[lo];
     v_end = V;
   }
-  for (; v < v_end;) {
-    // the run [lo, hi) of id v; 64 or more in sight hold a whole chunk
-    const unsigned k = lo + lane < N ? key[lo + lane] : (unsigned)V;
-    const unsigned long long same = __builtin_amdgcn_ballot_w64(k == v);
-    int n = __popcll(same);
-    if (n == 64) n = lower_bound(key + lo, N - lo, v + 1);
-    const int hi = lo + n;
-    if ((lo + CHUNK - 1) / CHUNK >= hi / CHUNK) {
+  // 64 sorted keys and their positions in sight, from `base` on: rows without a position cost no load
+  int base = lo;
+  unsigned keys = base + lane < N ? key[base + lane] : (unsigned)V;
+  int where = (int)(base + lane < N ? pos[base + lane] : 0u);
+  // Usually the rows' positions are few: then none has a whole chunk, and four positions' rows are loaded at a time, whichever row they belong to.
+  const unsigned last = BY_ROW ? v_end - 1 : __builtin_amdgcn_readfirstlane(min(key[stop - 1], (unsigned)V - 1));
+  const int m = __popcll(__builtin_amdgcn_ballot_w64(base + lane < N && keys <= last));
+  if (m < CHUNK) {
+    for (int d0 = 0; d0 < D; d0 += Piece<E, STEPS>::WIDTH) {
+      Piece<E, STEPS> acc(d0);
+      unsigned at = v;
+      for (int i = 0; i < m; i += 4) {
+        auto row = [&](int k) { return dout + (size_t)(unsigned)__builtin_amdgcn_readlane(where, min(i + k, m - 1)) * D; };
+        const T* const r[4] = {row(0), row(1), row(2), row(3)};
+        typename Piece<E, STEPS>::template Vec<T> x[4][STEPS];
+        acc.load(x, r, D);
+#pragma unroll
+        for (int k = 0; k < 4; k++) {
+          if (i + k >= m) break;
+          const unsigned id = __builtin_amdgcn_readlane(keys, i + k);
+          while (at != id) {
+            acc.store(dtable + (size_t)at * D, D, scale, accumulate);
+            acc.clear();
+            at = BY_ROW ? at + 1 : id;
+          }
+          acc.template add<T>(x[k]);
+        }
+      }
+      for (; at <= last; at++) {  // (by position: the last id alone)
+        acc.store(dtable + (size_t)at * D, D, scale, accumulate);
+        acc.clear();
+        if (!BY_ROW) break;
+      }
+    }
+    return;
+  }
+  while (v < v_end) {
+    if (lo - base >= 64 - CHUNK) {
+      base = lo;
+      keys = base + lane < N ? key[base + lane] : (unsigned)V;
+      where = (int)(base + lane < N ? pos[base + lane] : 0u);
+    }
+    // the run [lo, hi) of id v; one that reaches the end of what is in sight holds a whole chunk or ends there
+    const int n = __popcll(__builtin_amdgcn_ballot_w64(keys == v && base + lane >= lo));
+    const bool beyond = lo + n == base + 64;
+    const int hi = beyond ? lo + lower_bound(key + lo, N - lo, v + 1) : lo + n;
+    if ((lo + CHUNK - 1) / CHUNK >= hi / CHUNK) {  // (others: a workgroup's)
       for (int d0 = 0; d0 < D; d0 += Piece<E, STEPS>::WIDTH) {
         Piece<E, STEPS> acc(d0);
-        add_positions(acc, dout, D, pos, lo, hi);
+        if (beyond) add_positions(acc, dout, D, pos, lo, hi);
+        else add_lanes(acc, dout, D, where, lo - base, hi - lo);
         acc.store(dtable + (size_t)v * D, D, scale, accumulate);
       }
     }
@@ -540,7 +598,7 @@ __global__ __launch_bounds__(256) void embedding_direct_kernel(int N, int V, int
     for (int w = 0; w < DIRECT / 64; w++)
       for (unsigned long long m = hold[w]; m; m &= m - 1) {
         const T* const r[1] = {dout + (size_t)(w * 64 + __builtin_ctzll(m)) * D};
-        acc.add(r, D);
+        acc.add_rows(r, D);
       }
     acc.store(dtable + (size_t)v * D, D, scale, accumulate);
   }
