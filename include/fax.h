@@ -473,12 +473,13 @@ typedef struct FaxWindowDims {
  *   form         FAX_ATTENTION_*, as in FaxAttentionRoute.
  *   waves        bf16: wavefronts of a workgroup of the forward pass and dQ, 32 rows (queries of all heads of a key head) each: 4, or 1 for
  *                up to 32 rows.  fp32: 1, a tile of 32 rows.
+ *   fwd_groups, dq_groups    bf16: such sets of wavefronts in a workgroup, which have the same rows and share the keys: 2 where workgroups are no more than CUs.
  *   fwd_splits, dq_splits    runs of keys that a row's forward pass and its dQ are cut into, which a second kernel joins (1: none).
  *   sink_splits, key_splits  runs of queries that dK and dV are cut into (1: none): of the sinks (and the keys that share a tile with them), which
  *                every later query sees, and of the other keys.
  * Exposed so that a test can assert that its sizes run the form they are about. */
 typedef struct FaxWindowRoute {
-  int32_t form, waves, fwd_splits, dq_splits, sink_splits, key_splits;
+  int32_t form, waves, fwd_groups, dq_groups, fwd_splits, dq_splits, sink_splits, key_splits;
 } FaxWindowRoute;
 int fax_window_attention_route(const FaxWindowDims* dims, FaxWindowRoute* out);
 int fax_window_attention_workspace_bytes(const FaxWindowDims* dims, size_t* out);

@@ -92,7 +92,8 @@ class FaxWindowDims(C.Structure):
 
 
 class FaxWindowRoute(C.Structure):
-    _fields_ = [(n, C.c_int32) for n in ("form", "waves", "fwd_splits", "dq_splits", "sink_splits", "key_splits")]
+    _fields_ = [(n, C.c_int32) for n in ("form", "waves", "fwd_groups", "dq_groups", "fwd_splits", "dq_splits", "sink_splits",
+                                         "key_splits")]
 
 
 class FaxAdamWTensor(C.Structure):

@@ -26,12 +26,12 @@ struct WindowArgs {
 // How a size is run (kernels_window.hip), and where its parts lie in the workspace.
 struct WindowPlan {
   int form;                                    // FAX_ATTENTION_*
-  int waves, fwd_splits, dq_splits;            // wavefronts of a workgroup of rows; parts of a row's stream of keys
+  int waves, fwd_groups, dq_groups, fwd_splits, dq_splits;  // wavefronts of a group of a workgroup of rows, groups; parts of a row's stream of keys
   int kv_keys, sink_tiles, sink_splits, rest_splits;  // keys of a workgroup; tiles of them with sinks, parts of their streams of queries and of the others'
   size_t delta, part_o, part_ml, part_dq, part_ds, parts, total;
 };
-int window_fwd_mfma(const WindowArgs& a, int waves, int splits, float* part_o, void* part_ml, hipStream_t s);
-int window_dq_mfma(const WindowArgs& a, int waves, int splits, float* part_dq, float* part_ds, hipStream_t s);
+int window_fwd_mfma(const WindowArgs& a, int waves, int groups, int splits, float* part_o, void* part_ml, hipStream_t s);
+int window_dq_mfma(const WindowArgs& a, int waves, int groups, int splits, float* part_dq, float* part_ds, hipStream_t s);
 int window_dkv_keys(int dh);  // keys of a workgroup
 int window_dkv_mfma(const WindowArgs& a, const WindowPlan& p, float* parts, hipStream_t s);
 int window_fwd_f32(const WindowArgs& a, int splits, float* part_o, void* part_ml, hipStream_t s);

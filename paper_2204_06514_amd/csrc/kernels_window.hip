@@ -194,11 +194,16 @@ static int cut_stream(double blocks, long long tiles, const StreamCost& c, doubl
 //            tokens over 4096 keys, 32 on 8 x 128: one (8 workgroups) 149  4: 54  8: 30  16: 19  32: 13  64: 12;  four 150  55  32  22  26;  sixteen 150  57  61  68
 //   dQ       4096 of 2 on 1 x 128, all (64, up to 64 tiles), of both kernels 363  2: 302  4: 272  8: 269  16: 282;  1024 of 16 x 64, 300 38  2: 43
 //   dK, dV   the same two 363  262  212  192  201;  38  45  49
+// and by groups of wavefronts, us with one | with two (forward; backward, where only dQ has them):
+//   512 queries over 8192 keys, 16 on 4 x 128, 2048, of two (128 workgroups)  46.9 | 37.2; of four (256)  50.1 | 43.9;  four, x 64, 1024  21.2 | 18.4
+//   1024 of 16 x 64, 300 (128, 7 tiles)  12.9 | 11.8; 34.4 | 34.1    1000 of 15 on 5 x 80, 300 (120)  16.5 | 14.1; 47.4 | 45.0
+//   2048 of 16 x 64, 512 (256, 10 tiles)  16.5 | 14.5; 55.1 | 53.7   eight of 256 of 16 x 128, all (256, 4 tiles)  13.5 | 13.4; 37.7 | 39.8
+//   eight of 128 of 16 x 128, all (128, 2 tiles)  9.9 | 10.4; 23.4 | 25.5
 static WindowPlan window_plan(const FaxWindowDims& d) {
   WindowPlan p = {};
   p.form = FAX_ATTENTION_SCALAR;
   p.waves = 1;
-  p.fwd_splits = p.dq_splits = p.sink_splits = p.rest_splits = 1;
+  p.fwd_groups = p.dq_groups = p.fwd_splits = p.dq_splits = p.sink_splits = p.rest_splits = 1;
   const int unit = d.dtype == FAX_F32 ? 4 : 8, group = d.H / d.Hkv;
   const long long heads = (long long)d.B * d.Hkv, rows = (long long)d.Sq * group;
   if (d.dh % unit == 0 && d.dh <= 128 && strides_fit(d.q, unit) && strides_fit(d.kv, unit) && strides_fit(d.ctx, unit) && rows < (1 << 30)) {
@@ -218,6 +223,11 @@ static WindowPlan window_plan(const FaxWindowDims& d) {
     auto tiles = [&](long long keys) { return (keys + unit_keys - 1) / unit_keys; };
     p.fwd_splits = cut_stream(blocks, tiles(seen), fwd, row_bytes);
     p.dq_splits = cut_stream(blocks, tiles(seen), dq, row_bytes);
+    // Two groups of wavefronts to a workgroup where there is one to a CU: one group's tiles do not fill it, and adding up takes a microsecond or two.
+    if (p.waves == 4 && blocks <= 256) {
+      p.fwd_groups = p.fwd_splits == 1 && tiles(seen) >= 4 ? 2 : 1;
+      p.dq_groups = p.dq_splits == 1 && tiles(seen) >= 6 ? 2 : 1;
+    }
     // Keys: those among the sinks are seen by every later query, the others by a window's length of them.
     p.kv_keys = f32 ? 32 : window_dkv_keys(d.dh);
     const long long n = (d.Sk + p.kv_keys - 1) / p.kv_keys, sinks = d.sinks < d.Sk ? d.sinks : d.Sk, all = tiles((long long)d.Sq * group);
@@ -260,7 +270,7 @@ size_t window_ws_bytes(const FaxWindowDims& d) { return window_plan(d).total; }
 void window_route(const FaxWindowDims& d, FaxWindowRoute* out) {
   const WindowPlan p = window_plan(d);
   out->form = p.form;
-  out->waves = p.waves; out->fwd_splits = p.fwd_splits; out->dq_splits = p.dq_splits;
+  out->waves = p.waves; out->fwd_groups = p.fwd_groups; out->dq_groups = p.dq_groups; out->fwd_splits = p.fwd_splits; out->dq_splits = p.dq_splits;
   out->sink_splits = p.sink_splits; out->key_splits = p.rest_splits;
 }
 static bool on16(std::initializer_list<const void*> p) {
@@ -298,7 +308,7 @@ int window_fwd(const FaxWindowDims& d, const void* q, const void* k, const void*
     float* part_o = (float*)(w + p.part_o);
     float2* part_ml = (float2*)(w + p.part_ml);
     if (p.form == FAX_ATTENTION_F32) FAX_TRY(window_fwd_f32(a, p.fwd_splits, part_o, part_ml, s));
-    else FAX_TRY(window_fwd_mfma(a, p.waves, p.fwd_splits, part_o, part_ml, s));
+    else FAX_TRY(window_fwd_mfma(a, p.waves, p.fwd_groups, p.fwd_splits, part_o, part_ml, s));
     if (p.fwd_splits > 1) {
       const float log2e = 1.4426950408889634f;
       const dim3 grid((unsigned)(((long long)a.B * a.H * a.Sq + 3) / 4));
@@ -331,7 +341,7 @@ int window_bwd(const FaxWindowDims& d, const void* q, const void* k, const void*
       if (p.dq_splits > 1) hipLaunchKernelGGL(window_fold_dq_kernel<float>, dim3(row_blocks), dim3(256), 0, s, a, p.dq_splits, part_dq, (const float*)nullptr);
     } else {
       // dQ first: it also leaves delta, which dK and dV need
-      FAX_TRY(window_dq_mfma(a, p.waves, p.dq_splits, part_dq, part_ds, s));
+      FAX_TRY(window_dq_mfma(a, p.waves, p.dq_groups, p.dq_splits, part_dq, part_ds, s));
       if (p.dq_splits > 1) hipLaunchKernelGGL(window_fold_dq_kernel<bf16_t>, dim3(row_blocks), dim3(256), 0, s, a, p.dq_splits, part_dq, part_ds);
       FAX_TRY(window_dkv_mfma(a, p, parts, s));
     }

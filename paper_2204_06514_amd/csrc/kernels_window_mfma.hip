@@ -9,15 +9,15 @@ namespace fax {
 // PART: the workgroup has one of `splits` runs of the tiles and leaves its sums, undivided, with their reference point (in units of the
 // unscaled score) and their denominators, for window_join_kernel.
 // ---------------------------------------------------------------------------------------------
-template <int DW, bool EDGE, int WPG, bool PART>
-__global__ __launch_bounds__(64 * WPG, 2) void window_fwd_mfma_kernel(WindowArgs a, int n_tiles, int items, int splits, float* __restrict__ part_o,
+template <int DW, bool EDGE, int G, int WPG, bool PART>
+__global__ __launch_bounds__(64 * G * WPG, 2) void window_fwd_mfma_kernel(WindowArgs a, int n_tiles, int items, int splits, float* __restrict__ part_o,
                                                                       float2* __restrict__ part_ml) {
   constexpr int DH = row_width<DW>();  // row length in LDS
   constexpr int KS = DW / 16, DT = DW / 32, TB = TR * DH * 2;
   constexpr int N = 2 * KS;            // MFMAs per phase
   constexpr int LEAD = N < 8 ? N : 8;  // fragments in flight
   constexpr int NSEG = DH / 8 / WPG;   // 1 KB load instructions per wave per tile
-  extern __shared__ __attribute__((aligned(16))) char smem[];  // 2 x [K tile | V tile]
+  extern __shared__ __attribute__((aligned(16))) char smem_all[];  // to a group 2 x [K tile | V tile]
   int item = xcd_item(blockIdx.x, gridDim.x);
   if (item >= items) return;
   int split = 0;
@@ -25,14 +25,17 @@ __global__ __launch_bounds__(64 * WPG, 2) void window_fwd_mfma_kernel(WindowArgs
   const int tile_no = item % n_tiles, bh = item / n_tiles;
   const int b = bh / a.Hkv, hk = bh % a.Hkv;
   const WindowSeq sq(a, b);
-  const RowTile<WPG> rt(a, sq, b, hk, tile_no);
-  const int wave = rt.wave, lane = threadIdx.x & 63, g = lane >> 5;
+  const int wave_all = G * WPG == 1 ? 0 : __builtin_amdgcn_readfirstlane(threadIdx.x >> 6);
+  const int grp = G == 1 ? 0 : wave_all / WPG, wave = G == 1 ? wave_all : wave_all % WPG;
+  const RowTile<WPG> rt(a, sq, b, hk, tile_no, wave);
+  char* const smem = smem_all + grp * (4 * TB);
+  const int lane = threadIdx.x & 63, g = lane >> 5;
   const int hw = EDGE ? a.dh : DW, nch = hw / 8;
   const bf16_t* kb = strided_row((const bf16_t*)a.k, a.skv, b, 0, hk);
   const bf16_t* vb = strided_row((const bf16_t*)a.v, a.skv, b, 0, hk);
   const float scale = a.scale, c = scale * LOG2E;
   const unsigned sm = lds_addr(smem);
-  if (EDGE) clear_lds(smem, 4 * TB);
+  if (EDGE) clear_lds(smem_all, G * 4 * TB);
 
   const KeyTiles<TR> kt(KeyRanges(a, sq, rt.p0, rt.p1));
   const int u0 = PART ? (int)((long long)kt.n * split / splits) : 0, u1 = PART ? (int)((long long)kt.n * (split + 1) / splits) : kt.n;
@@ -143,31 +146,55 @@ __global__ __launch_bounds__(64 * WPG, 2) void window_fwd_mfma_kernel(WindowArgs
     __builtin_amdgcn_s_setprio(0);
   };
 
+  // (a group without a tile of its own loads the last, and meets the others' barriers)
   if (u0 < u1) {
-    load(kt.key(u0), 0);
+    load(kt.key(min(u0 + grp, u1 - 1)), 0);
     lds_dma_wait();
     __syncthreads();
     // Runs of tiles that take the masks (or that no row of the wave sees) and of tiles that do not, in loops of their own: one loop over both kinds
     // keeps the accumulators in two places, which does not fit the registers.
     const FullRun full = FullRun::keys(a, sq.k_len, rt.wp0, rt.wp1, kt);
     auto next = [&](int u) __attribute__((always_inline)) {
-      if (u + 1 < u1) load(kt.key(u + 1), (u - u0 + 1) & 1);
+      if (u + G < u1) load(kt.key(u + G), ((u - u0) / G + 1) & 1);
     };
     auto done = [&]() {
       lds_dma_wait();
       __syncthreads();
     };
-    for (int u = u0; u < u1;) {
-      for (; u < u1 && !full.has(u); u++) {
+    for (int u = u0 + grp; u < u1;) {
+      for (; u < u1 && !full.has(u); u += G) {
         next(u);
-        if (sees_any(a, sq.k_len, rt.wp0, rt.wp1, kt.key(u), TR)) tile(T_{}, kt.key(u), (u - u0) & 1);
+        if (sees_any(a, sq.k_len, rt.wp0, rt.wp1, kt.key(u), TR)) tile(T_{}, kt.key(u), (u - u0) / G & 1);
         done();
       }
-      for (; u < u1 && full.has(u); u++) {
+      for (; u < u1 && full.has(u); u += G) {
         next(u);
-        tile(F_{}, kt.key(u), (u - u0) & 1);
+        tile(F_{}, kt.key(u), (u - u0) / G & 1);
         done();
       }
+    }
+    if (G > 1)  // every group meets as many barriers as the one with the most tiles
+      for (int k = (u1 - u0 + G - 1) / G - (u1 - u0 - grp + G - 1) / G; k > 0; k--) __syncthreads();
+  }
+
+  if (G > 1) {
+    constexpr int U = DT * 4 + 1;
+    float* x = reinterpret_cast<float*>(smem_all);
+    if (grp) {
+      group_put<U>(x, wave_all - WPG, 0, oacc);
+      reinterpret_cast<float4*>(x)[((wave_all - WPG) * U + U - 1) * 64 + lane] = make_float4(m, l, 0.f, 0.f);
+    }
+    __syncthreads();
+    if (grp) return;
+#pragma unroll
+    for (int o = 0; o < G - 1; o++) {
+      const int slot = o * WPG + wave;
+      const float4 ml = reinterpret_cast<const float4*>(x)[(slot * U + U - 1) * 64 + lane];
+      const float mn = fmaxf(m, ml.x);
+      const float a0 = __builtin_amdgcn_exp2f((m - mn) * c), a1 = __builtin_amdgcn_exp2f((ml.x - mn) * c);
+      l = fmaf(l, a0, ml.y * a1);
+      m = mn;
+      group_add<U>(x, slot, 0, oacc, a0, a1);
     }
   }
 
@@ -204,15 +231,15 @@ __global__ __launch_bounds__(64 * WPG, 2) void window_fwd_mfma_kernel(WindowArgs
 // ---------------------------------------------------------------------------------------------
 // dQ, and delta = dctx . ctx by row.  The same tiles; per 32-key half S^T = K Q^T and dP^T = V dO^T, dS^T = P^T (dP^T - delta), dQ^T += K^T dS^T.
 // ---------------------------------------------------------------------------------------------
-template <int DW, bool EDGE, int WPG, bool PART>
-__global__ __launch_bounds__(64 * WPG, 2) void window_dq_mfma_kernel(WindowArgs a, int n_tiles, int items, int splits, float* __restrict__ part_dq,
+template <int DW, bool EDGE, int G, int WPG, bool PART>
+__global__ __launch_bounds__(64 * G * WPG, 2) void window_dq_mfma_kernel(WindowArgs a, int n_tiles, int items, int splits, float* __restrict__ part_dq,
                                                                      float* __restrict__ part_ds) {
   constexpr int DH = row_width<DW>();
   constexpr int KS = DW / 16, DT = DW / 32, TB = TR * DH * 2;
   constexpr int N1 = 2 * KS, N3 = 2 * DT, LEAD = N3;
   constexpr int NSEG = DH / 8 / WPG;
   static_assert(N1 % LEAD == 0, "slot plan");
-  extern __shared__ __attribute__((aligned(16))) char smem[];
+  extern __shared__ __attribute__((aligned(16))) char smem_all[];
   int item = xcd_item(blockIdx.x, gridDim.x);
   if (item >= items) return;
   int split = 0;
@@ -220,14 +247,17 @@ __global__ __launch_bounds__(64 * WPG, 2) void window_dq_mfma_kernel(WindowArgs 
   const int tile_no = item % n_tiles, bh = item / n_tiles;
   const int b = bh / a.Hkv, hk = bh % a.Hkv;
   const WindowSeq sq(a, b);
-  const RowTile<WPG> rt(a, sq, b, hk, tile_no);
-  const int wave = rt.wave, lane = threadIdx.x & 63, g = lane >> 5;
+  const int wave_all = G * WPG == 1 ? 0 : __builtin_amdgcn_readfirstlane(threadIdx.x >> 6);
+  const int grp = G == 1 ? 0 : wave_all / WPG, wave = G == 1 ? wave_all : wave_all % WPG;
+  const RowTile<WPG> rt(a, sq, b, hk, tile_no, wave);
+  char* const smem = smem_all + grp * (4 * TB);
+  const int lane = threadIdx.x & 63, g = lane >> 5;
   const int hw = EDGE ? a.dh : DW, nch = hw / 8;
   const bf16_t* kb = strided_row((const bf16_t*)a.k, a.skv, b, 0, hk);
   const bf16_t* vb = strided_row((const bf16_t*)a.v, a.skv, b, 0, hk);
   const float scale = a.scale, c = scale * LOG2E;
   const unsigned sm = lds_addr(smem);
-  if (EDGE) clear_lds(smem, 4 * TB);
+  if (EDGE) clear_lds(smem_all, G * 4 * TB);
   const KeyTiles<TR> kt(KeyRanges(a, sq, rt.p0, rt.p1));
   const int u0 = PART ? (int)((long long)kt.n * split / splits) : 0, u1 = PART ? (int)((long long)kt.n * (split + 1) / splits) : kt.n;
 
@@ -317,31 +347,50 @@ __global__ __launch_bounds__(64 * WPG, 2) void window_dq_mfma_kernel(WindowArgs 
     __builtin_amdgcn_s_setprio(0);
   };
 
+  // (a group without a tile of its own loads the last, and meets the others' barriers)
   if (u0 < u1) {
-    load(kt.key(u0), 0);
+    load(kt.key(min(u0 + grp, u1 - 1)), 0);
     lds_dma_wait();
     __syncthreads();
     // Runs of tiles that take the masks (or that no row of the wave sees) and of tiles that do not, in loops of their own: one loop over both kinds
     // keeps the accumulators in two places, which does not fit the registers.
     const FullRun full = FullRun::keys(a, sq.k_len, rt.wp0, rt.wp1, kt);
     auto next = [&](int u) __attribute__((always_inline)) {
-      if (u + 1 < u1) load(kt.key(u + 1), (u - u0 + 1) & 1);
+      if (u + G < u1) load(kt.key(u + G), ((u - u0) / G + 1) & 1);
     };
     auto done = [&]() {
       lds_dma_wait();
       __syncthreads();
     };
-    for (int u = u0; u < u1;) {
-      for (; u < u1 && !full.has(u); u++) {
+    for (int u = u0 + grp; u < u1;) {
+      for (; u < u1 && !full.has(u); u += G) {
         next(u);
-        if (sees_any(a, sq.k_len, rt.wp0, rt.wp1, kt.key(u), TR)) tile(T_{}, kt.key(u), (u - u0) & 1);
+        if (sees_any(a, sq.k_len, rt.wp0, rt.wp1, kt.key(u), TR)) tile(T_{}, kt.key(u), (u - u0) / G & 1);
         done();
       }
-      for (; u < u1 && full.has(u); u++) {
+      for (; u < u1 && full.has(u); u += G) {
         next(u);
-        tile(F_{}, kt.key(u), (u - u0) & 1);
+        tile(F_{}, kt.key(u), (u - u0) / G & 1);
         done();
       }
+    }
+    if (G > 1)  // every group meets as many barriers as the one with the most tiles
+      for (int k = (u1 - u0 + G - 1) / G - (u1 - u0 - grp + G - 1) / G; k > 0; k--) __syncthreads();
+  }
+  if (G > 1) {
+    constexpr int U = DT * 4 + 1;
+    float* x = reinterpret_cast<float*>(smem_all);
+    if (grp) {
+      group_put<U>(x, wave_all - WPG, 0, dq);
+      reinterpret_cast<float4*>(x)[((wave_all - WPG) * U + U - 1) * 64 + lane] = make_float4(ds_sum, 0.f, 0.f, 0.f);
+    }
+    __syncthreads();
+    if (grp) return;
+#pragma unroll
+    for (int o = 0; o < G - 1; o++) {
+      const int slot = o * WPG + wave;
+      ds_sum += reinterpret_cast<const float4*>(x)[(slot * U + U - 1) * 64 + lane].x;
+      group_add<U>(x, slot, 0, dq);
     }
   }
   // The probabilities of a row add up to one, so the sum of its dS is what delta, formed from ctx as it was rounded, lacks: dK gets it with that.
@@ -388,39 +437,41 @@ static int by_width(int dh, F f) {
   return dh < 64 ? f(I<64>{}, T_{}) : dh <= 96 ? f(I<96>{}, T_{}) : f(I<128>{}, T_{});
 }
 
-int window_fwd_mfma(const WindowArgs& a, int waves, int splits, float* part_o, void* part_ml, hipStream_t s) {
+int window_fwd_mfma(const WindowArgs& a, int waves, int groups, int splits, float* part_o, void* part_ml, hipStream_t s) {
   const int n_tiles = (int)(((long long)a.Sq * a.group + 32 * waves - 1) / (32 * waves));
   const long long items = (long long)n_tiles * a.B * a.Hkv * splits;
   return by_width(a.dh, [&](auto dw, auto edge) -> int {
     constexpr int DW = decltype(dw)::value;
     constexpr bool E = decltype(edge)::value;
-    constexpr size_t lds = 4 * (size_t)TR * row_width<DW>() * 2;
-    auto go = [&](auto wpg, auto part) -> int {
-      auto kern = window_fwd_mfma_kernel<DW, E, decltype(wpg)::value, decltype(part)::value>;
+    auto go = [&](auto g, auto wpg, auto part) -> int {
+      constexpr size_t lds = decltype(g)::value * 4 * (size_t)TR * row_width<DW>() * 2;
+      auto kern = window_fwd_mfma_kernel<DW, E, decltype(g)::value, decltype(wpg)::value, decltype(part)::value>;
       FAX_TRY(set_lds(kern, lds));
-      hipLaunchKernelGGL(kern, dim3(xcd_grid(items)), dim3(64 * waves), lds, s, a, n_tiles, (int)items, splits, part_o, (float2*)part_ml);
+      hipLaunchKernelGGL(kern, dim3(xcd_grid(items)), dim3(64 * groups * waves), lds, s, a, n_tiles, (int)items, splits, part_o, (float2*)part_ml);
       return FAX_OK;
     };
-    if (splits > 1) return waves == 1 ? go(I<1>{}, T_{}) : go(I<4>{}, T_{});
-    return waves == 1 ? go(I<1>{}, F_{}) : go(I<4>{}, F_{});
+    if (groups > 1) return go(I<2>{}, I<4>{}, F_{});
+    if (splits > 1) return waves == 1 ? go(I<1>{}, I<1>{}, T_{}) : go(I<1>{}, I<4>{}, T_{});
+    return waves == 1 ? go(I<1>{}, I<1>{}, F_{}) : go(I<1>{}, I<4>{}, F_{});
   });
 }
 
-int window_dq_mfma(const WindowArgs& a, int waves, int splits, float* part_dq, float* part_ds, hipStream_t s) {
+int window_dq_mfma(const WindowArgs& a, int waves, int groups, int splits, float* part_dq, float* part_ds, hipStream_t s) {
   const int n_tiles = (int)(((long long)a.Sq * a.group + 32 * waves - 1) / (32 * waves));
   const long long items = (long long)n_tiles * a.B * a.Hkv * splits;
   return by_width(a.dh, [&](auto dw, auto edge) -> int {
     constexpr int DW = decltype(dw)::value;
     constexpr bool E = decltype(edge)::value;
-    constexpr size_t lds = 4 * (size_t)TR * row_width<DW>() * 2;
-    auto go = [&](auto wpg, auto part) -> int {
-      auto kern = window_dq_mfma_kernel<DW, E, decltype(wpg)::value, decltype(part)::value>;
+    auto go = [&](auto g, auto wpg, auto part) -> int {
+      constexpr size_t lds = decltype(g)::value * 4 * (size_t)TR * row_width<DW>() * 2;
+      auto kern = window_dq_mfma_kernel<DW, E, decltype(g)::value, decltype(wpg)::value, decltype(part)::value>;
       FAX_TRY(set_lds(kern, lds));
-      hipLaunchKernelGGL(kern, dim3(xcd_grid(items)), dim3(64 * waves), lds, s, a, n_tiles, (int)items, splits, part_dq, part_ds);
+      hipLaunchKernelGGL(kern, dim3(xcd_grid(items)), dim3(64 * groups * waves), lds, s, a, n_tiles, (int)items, splits, part_dq, part_ds);
       return FAX_OK;
     };
-    if (splits > 1) return waves == 1 ? go(I<1>{}, T_{}) : go(I<4>{}, T_{});
-    return waves == 1 ? go(I<1>{}, F_{}) : go(I<4>{}, F_{});
+    if (groups > 1) return go(I<2>{}, I<4>{}, F_{});
+    if (splits > 1) return waves == 1 ? go(I<1>{}, I<1>{}, T_{}) : go(I<1>{}, I<4>{}, T_{});
+    return waves == 1 ? go(I<1>{}, I<1>{}, F_{}) : go(I<1>{}, I<4>{}, F_{});
   });
 }
 

@@ -49,6 +49,19 @@ def test_cut_streams(S, H, Hkv, window, sinks, dh, dtype):
     both(1, S, S, H, Hkv, dh, dtype, window, sinks)
 
 
+# Two groups of wavefronts with the same rows, which take every other tile: even and odd numbers of tiles, runs of whole ones among them, rows that see
+# one group's tiles only, workgroups with fewer tiles than groups.
+@pytest.mark.parametrize("dh", [40, 64, 80, 128])
+@pytest.mark.parametrize("B,S,H,Hkv,window,sinks,dq", [(8, 400, 8, 4, 200, 0, 1), (4, 1000, 8, 8, 300, 3, 2), (2, 1111, 14, 7, 333, 70, 2), (6, 600, 8, 8, 600, 0, 2)])
+def test_two_groups(B, S, H, Hkv, window, sinks, dq, dh):
+    r = route(B, S, S, H, Hkv, dh, "bf16", window, sinks)
+    assert (r.waves, r.fwd_groups, r.dq_groups, r.fwd_splits, r.dq_splits) == (4, 2, dq, 1, 1), forms(r)
+    short = torch.arange(B, dtype=torch.int32)
+    k_len = (S - 37 * short).clamp(min=1)
+    k_len[-1] = 50 if B > 3 else 0
+    both(B, S, S, H, Hkv, dh, "bf16", window, sinks, 3 * short, k_len)
+
+
 @pytest.mark.parametrize("dtype", ["bf16", "f32"])
 def test_sinks_alone_are_cut(dtype):
     B, S, H, window, sinks = 6, 1400, 8, 20, 5
