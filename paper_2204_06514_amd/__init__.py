@@ -421,17 +421,27 @@ def window_dims(q, k, window, sinks=0, ctx=None):
                          _strides(ctx) if ctx is not None else FaxStrides(0, 0, 0))
 
 
-def _laid_out(t, dims, name, strides):
-    """Address of a tensor that is laid out as `dims` says (an address is taken as it is)."""
+def _layouts(dims):
+    """(shape, strides) of q, kv and ctx as `dims` says, worked out once for as long as it says so."""
+    raw, known = bytes(dims), getattr(dims, "_known", None)
+    if known is None or known[0] != raw:
+        found = {}
+        for name, rows, heads in (("q", dims.Sq, dims.H), ("kv", dims.Sk, dims.Hkv), ("ctx", dims.Sq, dims.H)):
+            f = getattr(dims, name)
+            s = (f.batch, f.row, f.head)
+            found[name] = ((dims.B, rows, heads, dims.dh), (s if any(s) else (rows * heads * dims.dh, heads * dims.dh, dims.dh)) + (1,))
+        known = dims._known = (raw, found)
+    return known[1]
+
+
+def _laid_out(t, layout):
+    """Address of a tensor that is laid out like that (an address is taken as it is)."""
     if t is None or isinstance(t, int):
         return t
-    rows, heads = (dims.Sk, dims.Hkv) if name == "kv" else (dims.Sq, dims.H)
-    shape = (dims.B, rows, heads, dims.dh)
-    s = (strides.batch, strides.row, strides.head)
-    if s == (0, 0, 0):
-        s = (rows * heads * dims.dh, heads * dims.dh, dims.dh)
+    shape, strides = layout
     assert t.shape == shape, "a tensor of %s where dims say %s" % (tuple(t.shape), shape)
-    assert all(n == 1 or x == y for n, x, y in zip(shape, t.stride(), s + (1,))), "strides %s where dims.%s says %s" % (t.stride(), name, s)
+    s = t.stride()
+    assert s == strides or all(n == 1 or x == y for n, x, y in zip(shape, s, strides)), "strides %s where dims say %s" % (s, strides)
     return t.data_ptr()
 
 
@@ -449,15 +459,18 @@ def fax_window_attention_workspace_bytes(dims):
 
 def fax_window_attention_fwd(dims, q, k, v, q_pos, k_len, ctx, lse, ws, ws_bytes, stream=None):
     """q, k, v, ctx: laid out as `dims` says."""
-    at = lambda t, name: _laid_out(t, dims, name, getattr(dims, name))  # noqa: E731
-    _check(_lib.fax_window_attention_fwd(C.byref(dims), at(q, "q"), at(k, "kv"), at(v, "kv"), _ptr(q_pos), _ptr(k_len), at(ctx, "ctx"),
-                                         _ptr(lse), _ptr(ws), ws_bytes, _stream(stream)))
+    at = _layouts(dims)
+    _check(_lib.fax_window_attention_fwd(C.byref(dims), _laid_out(q, at["q"]), _laid_out(k, at["kv"]), _laid_out(v, at["kv"]),
+                                         _ptr(q_pos), _ptr(k_len), _laid_out(ctx, at["ctx"]), _ptr(lse), _ptr(ws), ws_bytes,
+                                         _stream(stream)))
 
 
 def fax_window_attention_bwd(dims, q, k, v, q_pos, k_len, ctx, lse, dctx, dq, dk, dv, ws, ws_bytes, stream=None):
-    at = lambda t, name: _laid_out(t, dims, name, getattr(dims, name))  # noqa: E731
-    _check(_lib.fax_window_attention_bwd(C.byref(dims), at(q, "q"), at(k, "kv"), at(v, "kv"), _ptr(q_pos), _ptr(k_len), at(ctx, "ctx"),
-                                         _ptr(lse), at(dctx, "ctx"), at(dq, "q"), at(dk, "kv"), at(dv, "kv"), _ptr(ws), ws_bytes,
+    at = _layouts(dims)
+    kv = at["kv"]
+    _check(_lib.fax_window_attention_bwd(C.byref(dims), _laid_out(q, at["q"]), _laid_out(k, kv), _laid_out(v, kv), _ptr(q_pos),
+                                         _ptr(k_len), _laid_out(ctx, at["ctx"]), _ptr(lse), _laid_out(dctx, at["ctx"]),
+                                         _laid_out(dq, at["q"]), _laid_out(dk, kv), _laid_out(dv, kv), _ptr(ws), ws_bytes,
                                          _stream(stream)))
 
 
