@@ -453,7 +453,7 @@ int fax_embedding_bwd(int dtype, int N, int V, int D, const int32_t* tokens, con
  * q_pos, k_len: int32 [B] on the device.  q_pos NULL: the queries are the last Sq of Sk positions (q_pos = Sk - Sq: 0 for a whole
  *   sequence, the newest token for Sq = 1).  k_len NULL: Sk.  k_len counts as 0 below zero and as Sk above; q_pos as -2^30 below that and as
  *   2^30 - Sq above that.  Rows of k and v from k_len on are not used, whatever they hold, and get zeros in dk and dv.
- * Sizes up to B * max(Sq, Sk) = 2^30, dh <= 256, window >= 1, sinks >= 0; H a multiple of Hkv.
+ * Sizes up to B Sq H = 2^27, B Sk Hkv = 2^27, B Hkv = 2^21, dh <= 256, window >= 1, sinks >= 0; H a multiple of Hkv.
  * q, k, v, ctx and their gradients may start at any element (not the 16-byte alignment of the other calls): rows that start on 16 bytes take the
  *   matrix cores where the head width is a multiple of 16 bytes and at most 128 (fax_window_attention_route tells), others scalar kernels.
  * lse may be NULL in the forward pass (inference).  Backward: ctx, lse as the forward pass left them; dq, dk, dv are overwritten.

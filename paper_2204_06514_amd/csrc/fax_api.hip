@@ -1179,10 +1179,13 @@ static int check_window(const FaxWindowDims* dims, FaxWindowDims* out) {
   if (d.window < 1 || d.sinks < 0) { set_error("window=%d must be >= 1, sinks=%d >= 0", d.window, d.sinks); return FAX_ERR_INVALID_ARG; }
   if (d.dh > 256) { set_error("head width %d exceeds 256", d.dh); return FAX_ERR_UNSUPPORTED; }
   const int64_t most = (int64_t)1 << 30;
-  if ((int64_t)d.B * d.Sq > most || (int64_t)d.B * d.Sk > most || (int64_t)d.B * d.Sq * d.H > 4 * most || (int64_t)d.B * d.Sk * d.Hkv > 4 * most) {
-    set_error("B*Sq or B*Sk exceeds 2^30, or with the heads 2^32");
+  if ((int64_t)d.B * d.Sq > most || (int64_t)d.B * d.Sk > most) { set_error("B*Sq or B*Sk exceeds 2^30"); return FAX_ERR_UNSUPPORTED; }
+  // (a launch has fewer than 2^32 threads: a tile of 32 rows or keys has 256)
+  if ((int64_t)d.B * d.Sq * d.H > most / 8 || (int64_t)d.B * d.Sk * d.Hkv > most / 8) {
+    set_error("B*Sq*H or B*Sk*Hkv exceeds 2^27");
     return FAX_ERR_UNSUPPORTED;
   }
+  if ((int64_t)d.B * d.Hkv > most / 512) { set_error("B*Hkv exceeds 2^21"); return FAX_ERR_UNSUPPORTED; }
   FAX_TRY(fill_strides(&d.q, "dims.q", d.Sq, d.H, d.dh));
   FAX_TRY(fill_strides(&d.kv, "dims.kv", d.Sk, d.Hkv, d.dh));
   FAX_TRY(fill_strides(&d.ctx, "dims.ctx", d.Sq, d.H, d.dh));
@@ -1273,7 +1276,7 @@ int fax_adamw_multi_step(int state, int count, const FaxAdamWTensor* tensors, co
     }
     if (t.lowp && misaligned(t.lowp)) { set_error("tensors[%d].lowp is not 16-byte aligned", i); return FAX_ERR_INVALID_ARG; }
     if (t.grad_dtype != FAX_F32 && t.grad_dtype != FAX_BF16) { set_error("tensors[%d].grad_dtype must be FAX_F32 or FAX_BF16", i); return FAX_ERR_INVALID_ARG; }
-    if (t.n > (size_t)1 << 42) { set_error("tensors[%d]: %zu elements", i, t.n); return FAX_ERR_UNSUPPORTED; }
+    if (t.n > (size_t)1 << 35) { set_error("tensors[%d]: %zu elements", i, t.n); return FAX_ERR_UNSUPPORTED; }
     if (state == FAX_STATE_E4M3) {
       if (!t.m_scale || !t.v_scale) { set_error("tensors[%d]: m_scale or v_scale is NULL", i); return FAX_ERR_INVALID_ARG; }
       if ((reinterpret_cast<uintptr_t>(t.m_scale) | reinterpret_cast<uintptr_t>(t.v_scale)) & 3) {

@@ -26,6 +26,13 @@ int hip_fail(hipError_t e, const char* what);
     if (s_ != FAX_OK) return s_; \
   } while (0)
 #define FAX_LAUNCH_CHECK(name) FAX_HIP(hipGetLastError())
+// A launch has fewer than 2^32 threads in a dimension: grids that may have more workgroups of up to 256 than that are folded at 2^23 (the last row
+// has some too many).
+inline dim3 wide_grid(unsigned long long blocks) {
+  const unsigned long long row = 1ull << 23;
+  return blocks <= row ? dim3((unsigned)blocks) : dim3((unsigned)row, (unsigned)((blocks + row - 1) / row));
+}
+__device__ __forceinline__ unsigned wide_block() { return blockIdx.y * gridDim.x + blockIdx.x; }
 
 // ---- GEMM -------------------------------------------------------------------------------
 enum { EPI_NONE = 0, EPI_GELU = 1, EPI_DGELU = 2 };

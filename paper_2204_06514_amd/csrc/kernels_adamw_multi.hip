@@ -228,7 +228,7 @@ int adamw_multi(int state, int count, const FaxAdamWTensor* tensors, const FaxAd
     const FaxAdamWTensor& x = tensors[t];
     if (x.n == 0) continue;
     const size_t chunks = (x.n + ADAM_CHUNK - 1) / ADAM_CHUNK;
-    if (b.count == MULTI_BATCH || b.first[b.count] + chunks > 0x7fffffffu) FAX_TRY(flush());
+    if (b.count == MULTI_BATCH || b.first[b.count] + chunks > 0xffffffu) FAX_TRY(flush());  // (fewer than 2^32 threads)
     MultiEntry& e = b.t[b.count];
     e.p = (float*)x.master; e.m = x.m; e.v = x.v; e.g = x.grad; e.lowp = (bf16_t*)x.lowp; e.n = x.n;
     e.m_scale = x.m_scale; e.v_scale = x.v_scale;

@@ -479,14 +479,15 @@ __global__ __launch_bounds__(256) void embedding_rows_kernel(int N, int V, int D
                                                              const uint32_t* __restrict__ pos, const T* __restrict__ dout, const float* __restrict__ sums,
                                                              float scale, int accumulate, float* __restrict__ dtable) {
   __shared__ float lds[3 * STEPS * E * 64];
-  if ((int)blockIdx.x < chunk_blocks) {
-    const int c = blockIdx.x;
+  const int block = (int)wide_block();
+  if (block < chunk_blocks) {
+    const int c = block;
     if (!whole_chunk(key, N, V, c)) return;
     if (whole_chunk(key, N, V, c - 1) && key[c * CHUNK - 1] == key[c * CHUNK]) return;  // not the first of its id
     long_row<T, E, STEPS>(N, D, c, key, pos, dout, sums, scale, accumulate, dtable, lds);
     return;
   }
-  const int item = ((int)blockIdx.x - chunk_blocks) * 4 + __builtin_amdgcn_readfirstlane(threadIdx.x >> 6);
+  const int item = (block - chunk_blocks) * 4 + __builtin_amdgcn_readfirstlane(threadIdx.x >> 6);
   const int lane = threadIdx.x & 63;
   unsigned v, v_end;
   int lo, stop = N;  // positions are looked for from lo on
@@ -573,7 +574,7 @@ __global__ __launch_bounds__(256) void embedding_rows_kernel(int N, int V, int D
 template <typename T, int E, int STEPS, bool BY_ROW>
 __global__ __launch_bounds__(256) void embedding_direct_kernel(int N, int V, int D, const int32_t* __restrict__ tokens, const T* __restrict__ dout, float scale,
                                                                int accumulate, float* __restrict__ dtable) {
-  const int item = blockIdx.x * 4 + __builtin_amdgcn_readfirstlane(threadIdx.x >> 6), lane = threadIdx.x & 63;
+  const int item = (int)wide_block() * 4 + __builtin_amdgcn_readfirstlane(threadIdx.x >> 6), lane = threadIdx.x & 63;
   if (item >= (BY_ROW ? V : N)) return;
   const int v = BY_ROW ? item : __builtin_amdgcn_readfirstlane(tokens[item]);
   if (!BY_ROW && (v < 0 || v >= V)) return;
@@ -628,7 +629,7 @@ size_t embedding_bwd_ws_bytes(int N, int V, int D) { return embedding_ws(N, V, D
 template <typename T, int E, int STEPS>
 static int embedding_bwd_t(int N, int V, int D, const int32_t* tokens, const T* dout, float scale, float* dtable, bool accumulate, char* ws, hipStream_t s) {
   if (N <= DIRECT) {
-    const dim3 grid(((accumulate ? N : V) + 3) / 4);
+    const dim3 grid = wide_grid(((accumulate ? N : V) + 3) / 4);
     if (accumulate) hipLaunchKernelGGL((embedding_direct_kernel<T, E, STEPS, false>), grid, dim3(256), 0, s, N, V, D, tokens, dout, scale, 1, dtable);
     else hipLaunchKernelGGL((embedding_direct_kernel<T, E, STEPS, true>), grid, dim3(256), 0, s, N, V, D, tokens, dout, scale, 0, dtable);
     FAX_LAUNCH_CHECK("embedding_bwd");
@@ -658,7 +659,7 @@ static int embedding_bwd_t(int N, int V, int D, const int32_t* tokens, const T* 
   const int chunks = N / CHUNK;
   hipLaunchKernelGGL((embedding_chunk_kernel<T, E, STEPS>), dim3((chunks + 3) / 4), dim3(256), 0, s, N, V, D, key, pos, dout, sums);
   const int items = ((accumulate ? N : V) + ROWS - 1) / ROWS;
-  const dim3 grid(chunks + (items + 3) / 4);
+  const dim3 grid = wide_grid(chunks + (items + 3) / 4);
   if (accumulate) hipLaunchKernelGGL((embedding_rows_kernel<T, E, STEPS, false>), grid, dim3(256), 0, s, N, V, D, chunks, key, pos, dout, sums, scale, 1, dtable);
   else hipLaunchKernelGGL((embedding_rows_kernel<T, E, STEPS, true>), grid, dim3(256), 0, s, N, V, D, chunks, key, pos, dout, sums, scale, 0, dtable);
   FAX_LAUNCH_CHECK("embedding_bwd");

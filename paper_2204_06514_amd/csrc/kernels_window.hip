@@ -13,7 +13,7 @@ template <typename T, int WHAT>  // 0 forward, 1 dQ, 2 dK and dV, 3 delta
 __global__ __launch_bounds__(256) void window_rows_kernel(WindowArgs a) {
   const int lane = threadIdx.x & 63;
   const int heads = WHAT == 2 ? a.Hkv : a.H, S = WHAT == 2 ? a.Sk : a.Sq;
-  const long long row = (long long)blockIdx.x * 4 + (threadIdx.x >> 6), rows = (long long)a.B * S * heads;
+  const long long row = (long long)wide_block() * 4 + (threadIdx.x >> 6), rows = (long long)a.B * S * heads;
   if (row >= rows) return;
   const int h = (int)(row % heads), i = (int)(row / heads % S), b = (int)(row / heads / S);
   if constexpr (WHAT == 0) window_fwd_row<MAX_R, T>(a, b, i, h, lane);
@@ -32,7 +32,7 @@ __global__ __launch_bounds__(256) void window_rows_kernel(WindowArgs a) {
 template <int WHAT>
 static int rows_launch(const WindowArgs& a, int dtype, hipStream_t s) {
   const long long rows = (long long)a.B * (WHAT == 2 ? (long long)a.Sk * a.Hkv : (long long)a.Sq * a.H);
-  const dim3 grid((unsigned)((rows + 3) / 4));
+  const dim3 grid = wide_grid((rows + 3) / 4);
   if (dtype == FAX_F32) hipLaunchKernelGGL((window_rows_kernel<float, WHAT>), grid, dim3(256), 0, s, a);
   else hipLaunchKernelGGL((window_rows_kernel<bf16_t, WHAT>), grid, dim3(256), 0, s, a);
   return FAX_OK;
@@ -236,9 +236,9 @@ static WindowPlan window_plan(const FaxWindowDims& d) {
     p.sink_tiles = (int)((sinks + p.kv_keys - 1) / p.kv_keys);
     p.rest_splits = cut_stream((double)((n - p.sink_tiles) * heads), stream, dkv, key_bytes * (n - p.sink_tiles) * heads);
     const long long chain = (stream + p.rest_splits - 1) / p.rest_splits;
-    if (p.sink_tiles > 0 && 2 * p.sink_tiles <= n) {  // as long as the others' parts
-      const long long parts = (all + chain - 1) / chain;
-      p.sink_splits = (int)(parts < 64 ? parts : 64);
+    if (p.sink_tiles > 0 && 2 * p.sink_tiles <= n) {  // as long as the others' parts, and no more of them than fill the chip several times over
+      const long long parts = (all + chain - 1) / chain, room = 1 + 2048 / (p.sink_tiles * heads);
+      p.sink_splits = (int)(parts < 64 && parts < room ? parts : room < 64 ? room : 64);
     } else {  // most keys are sinks: one kind of tile
       p.sink_tiles = 0;
       if (sinks > 0) p.rest_splits = cut_stream((double)(n * heads), all, dkv, key_bytes * n * heads);

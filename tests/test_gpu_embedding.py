@@ -105,3 +105,21 @@ def test_no_positions():
     assert (g == 3.0).all()
     fax.fax_embedding_bwd(fax.FAX_F32, 0, 5, 8, None, None, 1.0, g, 0, None, 0)
     assert (g == 0.0).all()
+
+
+@pytest.mark.parametrize("N,V", [(3, (1 << 26) + 7), (600, (1 << 28) + 5), (600, (1 << 30) - 3)])
+def test_more_rows_than_a_launch_has_threads(N, V):
+    """A table of one feature: the workgroups of all its rows do not fit one dimension of a launch."""
+    gen = torch.Generator().manual_seed(N)
+    t = torch.randint(0, V, (N,), generator=gen).to(torch.int32)
+    t[0], t[1], t[2] = V - 1, 0, V
+    dout = torch.randint(1, 100, (N, 1), generator=gen).to(torch.float32)
+    g = torch.full((V, 1), 7.0, device=DEV)
+    n = fax.fax_embedding_bwd_workspace_bytes(N, V, 1)
+    ws = torch.empty(n, dtype=torch.uint8, device=DEV)
+    fax.fax_embedding_bwd(fax.FAX_F32, N, V, 1, t.to(DEV), dout.to(DEV), 0.5, g, 0, ws, n)
+    at, where = torch.unique(t[t < V].long(), return_inverse=True)
+    sums = torch.zeros(len(at), dtype=torch.float64).index_add_(0, where, 0.5 * dout[t < V, 0].double())  # small halves: exact
+    assert (g[at.to(DEV), 0].cpu().double() == sums).all()
+    g[at.to(DEV)] = 0
+    assert torch.count_nonzero(g).item() == 0

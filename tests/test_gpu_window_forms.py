@@ -112,3 +112,27 @@ def test_offsets_beyond_32_bits():
     v.copy_(vv)
     got = run(q.to(DEV), k, v, None, 9, 2, backward=False)
     check(got, orc.window_attention(q.double(), kk.double(), vv.double(), 9, 2, dtype=TD["bf16"]))
+
+
+def test_more_rows_than_a_launch_has_threads():
+    """The scalar kernels at one feature, a wavefront to a row: the last rows and keys as they are by themselves."""
+    S, H, tail = (1 << 21) + 9, 33, 50
+    gen = torch.Generator(device=DEV).manual_seed(0)
+    q, k, v, d = (torch.randn(1, S, H, 1, generator=gen, device=DEV).bfloat16() for _ in range(4))
+
+    def run_one(q, k, v, d):
+        dims = fax.window_dims(q, k, 5)
+        n = fax.fax_window_attention_workspace_bytes(dims)
+        ws = torch.empty(n, dtype=torch.uint8, device=DEV)
+        ctx, lse, dq, dk, dv = torch.empty_like(q), torch.empty(1, H, q.shape[1], device=DEV), torch.empty_like(q), torch.empty_like(k), torch.empty_like(v)
+        fax.fax_window_attention_fwd(dims, q, k, v, None, None, ctx, lse, ws, n)
+        fax.fax_window_attention_bwd(dims, q, k, v, None, None, ctx, lse, d, dq, dk, dv, ws, n)
+        return ctx, lse.transpose(1, 2), dq, dk, dv
+
+    full = run_one(q, k, v, d)
+    part = run_one(*(t[:, -tail:].contiguous() for t in (q, k, v, d)))
+    for name, a, b in zip(("ctx", "lse", "dq", "dk", "dv"), full, part):
+        x, y = a[:, -tail + 8:].double(), b[:, 8:].double()
+        # fp32 sums of at most 5 terms below 100 in another order (5 * 2^-24 * 100 = 3e-5), which may move a bf16 value to its neighbour (2^-7 of it)
+        assert ((x - y).abs() <= 3e-5 + (y.abs() * 2 ** -7 if a.dtype == torch.bfloat16 else 0.0)).all(), name
+        assert torch.isfinite(a).all(), name

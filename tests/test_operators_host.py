@@ -161,3 +161,27 @@ def test_oracle_e4m3_is_torchs_format():
     r = orc.random20(7, 3, 1, 1 << 16)
     assert abs(r.mean() - 0.5) < 5e-3 and abs((r * r).mean() - 1 / 3) < 5e-3
     assert abs((r[1:] * r[:-1]).mean() - 0.25) < 5e-3
+
+
+def test_window_sizes_that_launches_do_not_reach():
+    size = fax.fax_window_attention_workspace_bytes
+    refused(UNSUPPORTED, "2^27", size, dims(B=1 << 12, Sq=1 << 14, H=4))
+    refused(UNSUPPORTED, "2^27", size, dims(B=1 << 12, Sk=1 << 15, H=2, Hkv=2))
+    refused(UNSUPPORTED, "2^21", size, dims(B=1 << 21, Sq=1, Sk=1, H=2, Hkv=2))
+    size(dims(B=1 << 20, Sq=1, Sk=1, H=2, Hkv=2))
+    size(dims(B=1, Sq=1 << 22, Sk=1 << 22, H=32, Hkv=32))
+
+
+def test_window_sinks_without_end_take_no_workspace_without_end():
+    """Half of the keys as sinks: their parts stay within some thousand tiles of 64 keys, dK and dV in fp32."""
+    for dtype in (fax.FAX_F32, fax.FAX_BF16):
+        for S, sinks in ((1 << 17, 1 << 16), (1 << 20, 1000), (40000, 20000)):
+            d = dims(B=1, Sq=S, Sk=S, H=8, Hkv=8, dh=128, window=1024, sinks=sinks, dtype=dtype)
+            delta = 4 * S * 8
+            assert fax.fax_window_attention_workspace_bytes(d) - delta < 2 * 4096 * 64 * 2 * 128 * 4
+
+
+def test_adamw_of_more_than_memory_holds():
+    one = (fax.FaxAdamWTensor * 1)(fax.FaxAdamWTensor(A, A, A, A, None, None, None, (1 << 35) + 1, fax.FAX_F32, 1))
+    hp = fax.FaxAdamW(1e-3, 0.9, 0.95, 1e-8, 0.1)
+    refused(UNSUPPORTED, "elements", fax.fax_adamw_multi_step, fax.FAX_STATE_F32, (one, 1), hp, 1, 0, stream=0)
