@@ -97,6 +97,9 @@ int embedding_fwd(int dtype, int N, int V, int D, const int32_t* tokens, const v
 //           thousands, is not one wavefront's chain.
 //   rows    one wavefront to ROWS rows of dtable.  Rows with whole chunks have a workgroup each: what comes before the first, the chunks' sums in four
 //           parts, what comes after the last.
+//   zeros   rows that no position holds are most of a table under a text (their frequencies fall like 1 / rank), and sorting leaves most of the chip
+//           idle.  The first digit's launches clear and set a byte for each row that is held; workgroups added to the later digits' launches write the
+//           zeros of the others, and the rows' kernel goes by position.
 // Up to DIRECT positions there is no sort: a wavefront finds a row's positions among all of them.
 // Ids outside [0, V) sort behind all others and are not looked at again.
 static constexpr int SORT_BITS = 8, BINS = 1 << SORT_BITS;
@@ -106,6 +109,7 @@ static constexpr int SMALL_KEYS = 4096;  // up to here one workgroup sorts in LD
 static constexpr int DIRECT = 512;
 static constexpr int CHUNK = 32;
 static constexpr int ROWS = 4;
+static constexpr int ZERO_ROWS = 8;
 
 struct SortPlan {
   int bits, passes;   // of a digit, digits
@@ -176,9 +180,42 @@ __device__ __forceinline__ unsigned scan256(unsigned x, unsigned* tmp) {
   return before + inc - x;
 }
 
+// What workgroups beyond the sort's do in a launch of it.  held: a byte for each row of the table, NULL: there are none.
+struct ZeroRows {
+  uint8_t* held;
+  float* table;
+  int D;
+  long long first, end;  // the first pass: bytes to clear (16 to a thread); later: rows to look at, ZERO_ROWS to a wavefront
+  unsigned blocks(int threads, bool rows) const { return (unsigned)((end - first + (rows ? threads / 64 * ZERO_ROWS : threads * 16) - 1) / (rows ? threads / 64 * ZERO_ROWS : threads * 16)); }
+};
+__device__ __forceinline__ void clear_held(const ZeroRows& z, int block) {
+  const long long at = ((long long)block * blockDim.x + threadIdx.x) * 16;
+  if (at < z.end) *reinterpret_cast<uint4*>(z.held + at) = make_uint4(0u, 0u, 0u, 0u);
+}
+__device__ __forceinline__ void zero_rows(const ZeroRows& z, int block) {
+  const int lane = threadIdx.x & 63;
+  const long long r0 = z.first + ((long long)block * (blockDim.x / 64) + __builtin_amdgcn_readfirstlane(threadIdx.x >> 6)) * ZERO_ROWS;
+  unsigned long long free_ = __builtin_amdgcn_ballot_w64(lane < ZERO_ROWS && r0 + lane < z.end && z.held[min(r0 + lane, z.end - 1)] == 0);
+  for (; free_; free_ &= free_ - 1) {
+    float* row = z.table + (size_t)(r0 + __builtin_ctzll(free_)) * z.D;
+    if (z.D % 4 == 0) {
+      Vec16<float> o;
+      o.raw = make_float4(0.f, 0.f, 0.f, 0.f);
+      for (int d = lane * 4; d < z.D; d += 256) o.store_nt(row + d);
+    } else {
+      for (int d = lane; d < z.D; d += 64) row[d] = 0.f;
+    }
+  }
+}
+
 // counts[run * BINS + digit].  in_key NULL: the first pass, keys from the tokens.
-__global__ __launch_bounds__(256) void sort_count_kernel(int N, int V, int shift, int bits, int run_keys, const int32_t* __restrict__ tokens,
-                                                         const uint32_t* __restrict__ in_key, uint32_t* __restrict__ counts) {
+__global__ __launch_bounds__(256) void sort_count_kernel(int N, int V, int shift, int bits, int run_keys, int runs, const int32_t* __restrict__ tokens,
+                                                         const uint32_t* __restrict__ in_key, uint32_t* __restrict__ counts, ZeroRows z) {
+  if ((int)blockIdx.x >= runs) {
+    if (in_key) zero_rows(z, blockIdx.x - runs);
+    else clear_held(z, blockIdx.x - runs);
+    return;
+  }
   __shared__ unsigned hist[BINS];
   hist[threadIdx.x] = 0;
   __syncthreads();
@@ -194,7 +231,11 @@ static constexpr int PLACE_WAVES = RUN_KEYS / 64;
 __global__ __launch_bounds__(64 * PLACE_WAVES) void sort_place_kernel(int N, int V, int shift, int bits, int run_keys, int runs, const int32_t* __restrict__ tokens,
                                                                       const uint32_t* __restrict__ in_key, const uint32_t* __restrict__ in_pos,
                                                                       const uint32_t* __restrict__ counts, uint32_t* __restrict__ out_key,
-                                                                      uint32_t* __restrict__ out_pos) {
+                                                                      uint32_t* __restrict__ out_pos, ZeroRows z) {
+  if ((int)blockIdx.x >= runs) {
+    zero_rows(z, blockIdx.x - runs);
+    return;
+  }
   constexpr int QUARTERS = PLACE_WAVES * 64 / BINS;
   __shared__ unsigned next[PLACE_WAVES][BINS];
   __shared__ unsigned part[2][QUARTERS][BINS], tmp[4];
@@ -240,6 +281,7 @@ __global__ __launch_bounds__(64 * PLACE_WAVES) void sort_place_kernel(int N, int
       [&](int k, unsigned& key, unsigned& pos) {
         key = in_key ? in_key[k0 + k] : key_of(tokens[k0 + k], V);
         pos = in_pos ? in_pos[k0 + k] : (unsigned)(k0 + k);
+        if (z.held && !in_key && key < (unsigned)V) z.held[key] = 1;  // (whoever holds it writes the same)
       },
       [&](unsigned to, unsigned key, unsigned pos) {
         out_key[to] = key;
@@ -606,7 +648,7 @@ __global__ __launch_bounds__(256) void embedding_direct_kernel(int N, int V, int
 }
 
 struct EmbeddingWs {
-  size_t key[2], pos[2], counts, sums, total;
+  size_t key[2], pos[2], counts, held, sums, total;
 };
 static EmbeddingWs embedding_ws(int N, int V, int D) {
   const SortPlan p = sort_plan(N, V);
@@ -619,6 +661,7 @@ static EmbeddingWs embedding_ws(int N, int V, int D) {
       w.pos[i] = take((size_t)N * 4);
     }
     w.counts = take((size_t)p.runs * BINS * 4);
+    w.held = take(V);
     w.sums = take((size_t)(N / CHUNK) * D * 4);
   }
   w.total = o ? o : 256;  // (never none: a caller's empty allocation has no address)
@@ -638,6 +681,7 @@ static int embedding_bwd_t(int N, int V, int D, const int32_t* tokens, const T* 
   const SortPlan p = sort_plan(N, V);
   const EmbeddingWs w = embedding_ws(N, V, D);
   uint32_t *key = nullptr, *pos = nullptr;
+  bool zeros = false;  // of rows without a position: written beside the sort
   if (N <= SMALL_KEYS) {
     key = (uint32_t*)(ws + w.key[0]);
     pos = (uint32_t*)(ws + w.pos[0]);
@@ -647,10 +691,20 @@ static int embedding_bwd_t(int N, int V, int D, const int32_t* tokens, const T* 
     hipLaunchKernelGGL(sort_small_kernel, dim3(1), dim3(1024), lds, s, N, V, p.bits, p.passes, tokens, key, pos);
   } else {
     uint32_t* counts = (uint32_t*)(ws + w.counts);
+    zeros = !accumulate && p.passes > 1;
+    ZeroRows z = {zeros ? (uint8_t*)(ws + w.held) : nullptr, dtable, D, 0, zeros ? V : 0};
+    const int shares = 2 * (p.passes - 1);
     for (int i = 0; i < p.passes; i++) {
       uint32_t *ok = (uint32_t*)(ws + w.key[i & 1]), *op = (uint32_t*)(ws + w.pos[i & 1]);
-      hipLaunchKernelGGL(sort_count_kernel, dim3(p.runs), dim3(256), 0, s, N, V, i * p.bits, p.bits, p.run_keys, tokens, key, counts);
-      hipLaunchKernelGGL(sort_place_kernel, dim3(p.runs), dim3(64 * PLACE_WAVES), 0, s, N, V, i * p.bits, p.bits, p.run_keys, p.runs, tokens, key, pos, counts, ok, op);
+      auto share = [&](int k) {  // of the rows, for one of the later digits' launches
+        z.first = zeros && k >= 0 ? (long long)V * k / shares : 0;
+        z.end = zeros && k >= 0 ? (long long)V * (k + 1) / shares : 0;
+      };
+      if (i > 0) share(2 * i - 2);
+      hipLaunchKernelGGL(sort_count_kernel, dim3(p.runs + z.blocks(256, i > 0)), dim3(256), 0, s, N, V, i * p.bits, p.bits, p.run_keys, p.runs, tokens, key, counts, z);
+      share(i > 0 ? 2 * i - 1 : -1);
+      hipLaunchKernelGGL(sort_place_kernel, dim3(p.runs + z.blocks(64 * PLACE_WAVES, true)), dim3(64 * PLACE_WAVES), 0, s, N, V, i * p.bits, p.bits, p.run_keys, p.runs,
+                         tokens, key, pos, counts, ok, op, z);
       key = ok;
       pos = op;
     }
@@ -658,9 +712,10 @@ static int embedding_bwd_t(int N, int V, int D, const int32_t* tokens, const T* 
   float* sums = (float*)(ws + w.sums);
   const int chunks = N / CHUNK;
   hipLaunchKernelGGL((embedding_chunk_kernel<T, E, STEPS>), dim3((chunks + 3) / 4), dim3(256), 0, s, N, V, D, key, pos, dout, sums);
-  const int items = ((accumulate ? N : V) + ROWS - 1) / ROWS;
+  const bool by_row = !accumulate && !zeros;
+  const int items = ((by_row ? V : N) + ROWS - 1) / ROWS;
   const dim3 grid = wide_grid(chunks + (items + 3) / 4);
-  if (accumulate) hipLaunchKernelGGL((embedding_rows_kernel<T, E, STEPS, false>), grid, dim3(256), 0, s, N, V, D, chunks, key, pos, dout, sums, scale, 1, dtable);
+  if (!by_row) hipLaunchKernelGGL((embedding_rows_kernel<T, E, STEPS, false>), grid, dim3(256), 0, s, N, V, D, chunks, key, pos, dout, sums, scale, accumulate, dtable);
   else hipLaunchKernelGGL((embedding_rows_kernel<T, E, STEPS, true>), grid, dim3(256), 0, s, N, V, D, chunks, key, pos, dout, sums, scale, 0, dtable);
   FAX_LAUNCH_CHECK("embedding_bwd");
   return FAX_OK;
