@@ -409,11 +409,16 @@ struct Piece {
   }
 };
 
-// acc += the rows of the positions in lanes from .. from + n - 1 of `mine`, four in flight.
-template <typename T, int E, int STEPS>
+// acc += the rows of the positions in lanes from .. from + n - 1 of `mine`, four (eight) in flight.
+template <bool EIGHT = false, typename T, int E, int STEPS>
 __device__ __forceinline__ void add_lanes(Piece<E, STEPS>& acc, const T* __restrict__ dout, int D, int mine, int from, int n) {
   auto row = [&](int i) { return dout + (size_t)(unsigned)__builtin_amdgcn_readlane(mine, from + i) * D; };
   int i = 0;
+  if constexpr (EIGHT)
+    for (; i + 8 <= n; i += 8) {
+      const T* const r[8] = {row(i), row(i + 1), row(i + 2), row(i + 3), row(i + 4), row(i + 5), row(i + 6), row(i + 7)};
+      acc.add_rows(r, D);
+    }
   for (; i + 4 <= n; i += 4) {
     const T* const r[4] = {row(i), row(i + 1), row(i + 2), row(i + 3)};
     acc.add_rows(r, D);
@@ -438,20 +443,19 @@ __device__ __forceinline__ bool whole_chunk(const uint32_t* __restrict__ key, in
   return c >= 0 && k + CHUNK <= N && key[k] < (unsigned)V && key[k] == key[k + CHUNK - 1];
 }
 
-template <typename T, int E, int STEPS>
-__global__ __launch_bounds__(256) void embedding_chunk_kernel(int N, int V, int D, const uint32_t* __restrict__ key, const uint32_t* __restrict__ pos,
-                                                              const T* __restrict__ dout, float* __restrict__ sums) {
-  const int c = blockIdx.x * 4 + (threadIdx.x >> 6);
+// A wavefront to a piece of a chunk's sum.  (All of the row to a wavefront is three times fewer of them at 768 features, each waiting for loads most of
+// its time.)
+template <typename T, int E>
+__global__ __launch_bounds__(256) void embedding_chunk_kernel(int N, int V, int D, Divider pieces, const uint32_t* __restrict__ key,
+                                                              const uint32_t* __restrict__ pos, const T* __restrict__ dout, float* __restrict__ sums) {
+  const unsigned item = wide_block() * 4u + __builtin_amdgcn_readfirstlane(threadIdx.x >> 6), chunk = pieces(item);
+  const int c = (int)chunk;
   if (!whole_chunk(key, N, V, c)) return;
-  for (int d0 = 0; d0 < D; d0 += Piece<E, STEPS>::WIDTH) {
-    Piece<E, STEPS> acc(d0);
-    add_positions(acc, dout, D, pos, c * CHUNK, (c + 1) * CHUNK);
+  Piece<E, 1> acc((int)(item - chunk * pieces.d) * Piece<E, 1>::WIDTH);
+  add_lanes<true>(acc, dout, D, (int)pos[c * CHUNK + (threadIdx.x & (CHUNK - 1))], 0, CHUNK);
+  if (acc.at[0] < D)
 #pragma unroll
-    for (int s = 0; s < STEPS; s++)
-      if (acc.at[s] < D)
-#pragma unroll
-        for (int e = 0; e < E; e++) sums[(size_t)c * D + acc.at[s] + e] = acc.x[s][e];
-  }
+    for (int e = 0; e < E; e++) sums[(size_t)c * D + acc.at[0] + e] = acc.x[0][e];
 }
 
 // The first of n sorted keys that is at least v: 64 candidates at a time.
@@ -531,35 +535,42 @@ __global__ __launch_bounds__(256) void embedding_rows_kernel(int N, int V, int D
   }
   const int item = (block - chunk_blocks) * 4 + __builtin_amdgcn_readfirstlane(threadIdx.x >> 6);
   const int lane = threadIdx.x & 63;
-  unsigned v, v_end;
-  int lo, stop = N;  // positions are looked for from lo on
+  unsigned v, v_end, last;
+  int lo, base, stop = N;  // positions are looked for from lo on; 64 sorted keys and their positions are in sight, from `base` on
+  unsigned keys;
+  int where;
+  auto look = [&]() __attribute__((always_inline)) {
+    keys = base + lane < N ? key[base + lane] : (unsigned)V;
+    where = (int)(base + lane < N ? pos[base + lane] : 0u);
+  };
   if (BY_ROW) {
     if ((long long)item * ROWS >= V) return;
     v = item * ROWS;
     v_end = min((unsigned)V, v + ROWS);
-    lo = lower_bound(key, N, v);
+    last = v_end - 1;
+    lo = base = lower_bound(key, N, v);
+    look();
   } else {
     if ((long long)item * ROWS >= N) return;
-    lo = item * ROWS;
-    stop = min(N, lo + ROWS);
-    if (lo > 0)  // positions of an id that begins before: not this wavefront's
-      while (lo < stop && key[lo] == key[lo - 1]) lo++;
-    if (lo >= stop || key[lo] >= (unsigned)V) return;
-    v = key[lo];
+    base = item * ROWS;
+    stop = min(N, base + ROWS);
+    const unsigned before = lane < ROWS && base + lane > 0 && base + lane < N ? key[base + lane - 1] : (unsigned)V;
+    look();
+    const unsigned long long starts = __builtin_amdgcn_ballot_w64(lane < stop - base && keys != before);
+    if (starts == 0) return;  // positions of an id that begins before: not this wavefront's
+    lo = base + __builtin_ctzll(starts);
+    v = __builtin_amdgcn_readlane(keys, lo - base);
+    if (v >= (unsigned)V) return;
+    last = min((unsigned)__builtin_amdgcn_readlane(keys, stop - base - 1), (unsigned)V - 1);
     v_end = V;
   }
-  // 64 sorted keys and their positions in sight, from `base` on: rows without a position cost no load
-  int base = lo;
-  unsigned keys = base + lane < N ? key[base + lane] : (unsigned)V;
-  int where = (int)(base + lane < N ? pos[base + lane] : 0u);
   // Usually the rows' positions are few: then none has a whole chunk, and four positions' rows are loaded at a time, whichever row they belong to.
-  const unsigned last = BY_ROW ? v_end - 1 : __builtin_amdgcn_readfirstlane(min(key[stop - 1], (unsigned)V - 1));
   const int m = __popcll(__builtin_amdgcn_ballot_w64(base + lane < N && keys <= last));
   if (m < CHUNK) {
     for (int d0 = 0; d0 < D; d0 += Piece<E, STEPS>::WIDTH) {
       Piece<E, STEPS> acc(d0);
       unsigned at = v;
-      for (int i = 0; i < m; i += 4) {
+      for (int i = lo - base; i < m; i += 4) {
         auto row = [&](int k) { return dout + (size_t)(unsigned)__builtin_amdgcn_readlane(where, min(i + k, m - 1)) * D; };
         const T* const r[4] = {row(0), row(1), row(2), row(3)};
         typename Piece<E, STEPS>::template Vec<T> x[4][STEPS];
@@ -587,8 +598,7 @@ __global__ __launch_bounds__(256) void embedding_rows_kernel(int N, int V, int D
   while (v < v_end) {
     if (lo - base >= 64 - CHUNK) {
       base = lo;
-      keys = base + lane < N ? key[base + lane] : (unsigned)V;
-      where = (int)(base + lane < N ? pos[base + lane] : 0u);
+      look();
     }
     // the run [lo, hi) of id v; one that reaches the end of what is in sight holds a whole chunk or ends there
     const int n = __popcll(__builtin_amdgcn_ballot_w64(keys == v && base + lane >= lo));
@@ -711,7 +721,8 @@ static int embedding_bwd_t(int N, int V, int D, const int32_t* tokens, const T* 
   }
   float* sums = (float*)(ws + w.sums);
   const int chunks = N / CHUNK;
-  hipLaunchKernelGGL((embedding_chunk_kernel<T, E, STEPS>), dim3((chunks + 3) / 4), dim3(256), 0, s, N, V, D, key, pos, dout, sums);
+  const Divider pieces((D + Piece<E, 1>::WIDTH - 1) / Piece<E, 1>::WIDTH);
+  hipLaunchKernelGGL((embedding_chunk_kernel<T, E>), wide_grid(((unsigned long long)chunks * pieces.d + 3) / 4), dim3(256), 0, s, N, V, D, pieces, key, pos, dout, sums);
   const bool by_row = !accumulate && !zeros;
   const int items = ((by_row ? V : N) + ROWS - 1) / ROWS;
   const dim3 grid = wide_grid(chunks + (items + 3) / 4);
