@@ -95,7 +95,7 @@ int embedding_fwd(int dtype, int N, int V, int D, const int32_t* tokens, const v
 //           by bit (ballots).
 //   chunks  of CHUNK sorted positions that all hold the same id are added up into a row of scratch each, so that a frequent id, of which a text has
 //           thousands, is not one wavefront's chain.
-//   rows    one wavefront to ROWS rows of dtable.  Rows with whole chunks have a workgroup each: what comes before the first, the chunks' sums in four
+//   rows    a wavefront to pieces of a few rows of dtable.  Rows with whole chunks have a workgroup to a piece: what comes before the first, the chunks' sums in four
 //           parts, what comes after the last.
 //   zeros   rows that no position holds are most of a table under a text (their frequencies fall like 1 / rank), and sorting leaves most of the chip
 //           idle.  The first digit's launches clear and set a byte for each row that is held; workgroups added to the later digits' launches write the
@@ -108,8 +108,7 @@ static constexpr int MOST_RUNS = 256;
 static constexpr int SMALL_KEYS = 4096;  // up to here one workgroup sorts in LDS
 static constexpr int DIRECT = 512;
 static constexpr int CHUNK = 32;
-static constexpr int ROWS = 4;
-static constexpr int ZERO_ROWS = 8;
+static constexpr int ZERO_ROWS = 8, IN_FLIGHT = 4;
 
 struct SortPlan {
   int bits, passes;   // of a digit, digits
@@ -474,9 +473,9 @@ __device__ __forceinline__ int lower_bound(const uint32_t* __restrict__ key, int
   return __builtin_amdgcn_readfirstlane(lo);
 }
 
-// The row of an id that has whole chunks, the first of them c: a workgroup.
-template <typename T, int E, int STEPS>
-__device__ __forceinline__ void long_row(int N, int D, int c, const uint32_t* __restrict__ key, const uint32_t* __restrict__ pos, const T* __restrict__ dout,
+// A piece of the row of an id that has whole chunks, the first of them c: a workgroup.
+template <typename T, int E>
+__device__ __forceinline__ void long_row(int N, int D, int c, int piece, const uint32_t* __restrict__ key, const uint32_t* __restrict__ pos, const T* __restrict__ dout,
                                          const float* __restrict__ sums, float scale, bool accumulate, float* __restrict__ dtable, float* lds) {
   const unsigned v = key[c * CHUNK];
   const int wave = __builtin_amdgcn_readfirstlane(threadIdx.x >> 6), lane = threadIdx.x & 63;
@@ -485,55 +484,50 @@ __device__ __forceinline__ void long_row(int N, int D, int c, const uint32_t* __
   const int lo = c * CHUNK - __popcll(__builtin_amdgcn_ballot_w64(lane < CHUNK && back >= 0 && key[max(back, 0)] == v));
   const int hi = c * CHUNK + lower_bound(key + c * CHUNK, N - c * CHUNK, v + 1);
   const int c1 = hi / CHUNK, per = (c1 - c + 3) / 4;
-  for (int d0 = 0; d0 < D; d0 += Piece<E, STEPS>::WIDTH) {
-    Piece<E, STEPS> acc(d0);
-    if (wave == 0) add_positions(acc, dout, D, pos, lo, c * CHUNK);
-    int k = c + wave * per;
-    const int end = min(c1, k + per);
-    auto row = [&](int i) { return sums + (size_t)i * D; };
-    for (; k + 4 <= end; k += 4) {
-      const float* const r[4] = {row(k), row(k + 1), row(k + 2), row(k + 3)};
-      acc.add_rows(r, D);
-    }
-    for (; k < end; k++) {
-      const float* const r[1] = {row(k)};
-      acc.add_rows(r, D);
-    }
-    if (wave == 3) add_positions(acc, dout, D, pos, c1 * CHUNK, hi);
-    __syncthreads();
-    if (wave > 0)
+  Piece<E, 1> acc(piece * Piece<E, 1>::WIDTH);
+  if (wave == 0) add_positions(acc, dout, D, pos, lo, c * CHUNK);
+  int k = c + wave * per;
+  const int end = min(c1, k + per);
+  auto row = [&](int i) { return sums + (size_t)i * D; };
+  for (; k + 8 <= end; k += 8) {
+    const float* const r[8] = {row(k), row(k + 1), row(k + 2), row(k + 3), row(k + 4), row(k + 5), row(k + 6), row(k + 7)};
+    acc.add_rows(r, D);
+  }
+  for (; k < end; k++) {
+    const float* const r[1] = {row(k)};
+    acc.add_rows(r, D);
+  }
+  if (wave == 3) add_positions(acc, dout, D, pos, c1 * CHUNK, hi);
+  if (wave > 0)
 #pragma unroll
-      for (int s = 0; s < STEPS; s++)
+    for (int e = 0; e < E; e++) lds[((wave - 1) * E + e) * 64 + lane] = acc.x[0][e];
+  __syncthreads();
+  if (wave == 0) {
+    for (int w = 0; w < 3; w++)
 #pragma unroll
-        for (int e = 0; e < E; e++) lds[((wave - 1) * STEPS * E + s * E + e) * 64 + lane] = acc.x[s][e];
-    __syncthreads();
-    if (wave == 0) {
-      for (int w = 0; w < 3; w++)
-#pragma unroll
-        for (int s = 0; s < STEPS; s++)
-#pragma unroll
-          for (int e = 0; e < E; e++) acc.x[s][e] += lds[(w * STEPS * E + s * E + e) * 64 + lane];
-      acc.store(dtable + (size_t)v * D, D, scale, accumulate);
-    }
+      for (int e = 0; e < E; e++) acc.x[0][e] += lds[(w * E + e) * 64 + lane];
+    acc.store(dtable + (size_t)v * D, D, scale, accumulate);
   }
 }
 
-// The first `chunk_blocks` workgroups: rows with whole chunks.  The others, a wavefront each: BY_ROW, ROWS rows of the table, with zeros where no
-// position holds them; otherwise ROWS sorted positions, of which the first of an id adds (what comes without an id's first is another's).
-template <typename T, int E, int STEPS, bool BY_ROW>
-__global__ __launch_bounds__(256) void embedding_rows_kernel(int N, int V, int D, int chunk_blocks, const uint32_t* __restrict__ key,
+// The first `chunk_blocks` workgroups: pieces of rows with whole chunks.  The others, a wavefront to a piece: BY_ROW, of `per` rows of the table, with zeros
+// where no position holds them; otherwise of `per` sorted positions, of which the first of an id adds (what comes without an id's first is another's).
+template <typename T, int E, bool BY_ROW>
+__global__ __launch_bounds__(256) void embedding_rows_kernel(int N, int V, int D, int per, int chunk_blocks, Divider pieces, const uint32_t* __restrict__ key,
                                                              const uint32_t* __restrict__ pos, const T* __restrict__ dout, const float* __restrict__ sums,
                                                              float scale, int accumulate, float* __restrict__ dtable) {
-  __shared__ float lds[3 * STEPS * E * 64];
+  __shared__ float lds[3 * E * 64];
   const int block = (int)wide_block();
   if (block < chunk_blocks) {
-    const int c = block;
+    const unsigned at = pieces((unsigned)block);
+    const int c = (int)at;
     if (!whole_chunk(key, N, V, c)) return;
     if (whole_chunk(key, N, V, c - 1) && key[c * CHUNK - 1] == key[c * CHUNK]) return;  // not the first of its id
-    long_row<T, E, STEPS>(N, D, c, key, pos, dout, sums, scale, accumulate, dtable, lds);
+    long_row<T, E>(N, D, c, block - (int)(at * pieces.d), key, pos, dout, sums, scale, accumulate, dtable, lds);
     return;
   }
-  const int item = (block - chunk_blocks) * 4 + __builtin_amdgcn_readfirstlane(threadIdx.x >> 6);
+  const unsigned place = (unsigned)(block - chunk_blocks) * 4u + __builtin_amdgcn_readfirstlane(threadIdx.x >> 6);
+  const int item = (int)pieces(place), d0 = (int)(place - item * pieces.d) * Piece<E, 1>::WIDTH;
   const int lane = threadIdx.x & 63;
   unsigned v, v_end, last;
   int lo, base, stop = N;  // positions are looked for from lo on; 64 sorted keys and their positions are in sight, from `base` on
@@ -544,17 +538,17 @@ __global__ __launch_bounds__(256) void embedding_rows_kernel(int N, int V, int D
     where = (int)(base + lane < N ? pos[base + lane] : 0u);
   };
   if (BY_ROW) {
-    if ((long long)item * ROWS >= V) return;
-    v = item * ROWS;
-    v_end = min((unsigned)V, v + ROWS);
+    if ((long long)item * per >= V) return;
+    v = item * per;
+    v_end = min((unsigned)V, v + per);
     last = v_end - 1;
     lo = base = lower_bound(key, N, v);
     look();
   } else {
-    if ((long long)item * ROWS >= N) return;
-    base = item * ROWS;
-    stop = min(N, base + ROWS);
-    const unsigned before = lane < ROWS && base + lane > 0 && base + lane < N ? key[base + lane - 1] : (unsigned)V;
+    if ((long long)item * per >= N) return;
+    base = item * per;
+    stop = min(N, base + per);
+    const unsigned before = lane < per && base + lane > 0 && base + lane < N ? key[base + lane - 1] : (unsigned)V;
     look();
     const unsigned long long starts = __builtin_amdgcn_ballot_w64(lane < stop - base && keys != before);
     if (starts == 0) return;  // positions of an id that begins before: not this wavefront's
@@ -567,31 +561,30 @@ __global__ __launch_bounds__(256) void embedding_rows_kernel(int N, int V, int D
   // Usually the rows' positions are few: then none has a whole chunk, and four positions' rows are loaded at a time, whichever row they belong to.
   const int m = __popcll(__builtin_amdgcn_ballot_w64(base + lane < N && keys <= last));
   if (m < CHUNK) {
-    for (int d0 = 0; d0 < D; d0 += Piece<E, STEPS>::WIDTH) {
-      Piece<E, STEPS> acc(d0);
-      unsigned at = v;
-      for (int i = lo - base; i < m; i += 4) {
-        auto row = [&](int k) { return dout + (size_t)(unsigned)__builtin_amdgcn_readlane(where, min(i + k, m - 1)) * D; };
-        const T* const r[4] = {row(0), row(1), row(2), row(3)};
-        typename Piece<E, STEPS>::template Vec<T> x[4][STEPS];
-        acc.load(x, r, D);
+    Piece<E, 1> acc(d0);
+    unsigned at = v;
+    for (int i = lo - base; i < m; i += IN_FLIGHT) {
+      const T* r[IN_FLIGHT];
 #pragma unroll
-        for (int k = 0; k < 4; k++) {
-          if (i + k >= m) break;
-          const unsigned id = __builtin_amdgcn_readlane(keys, i + k);
-          while (at != id) {
-            acc.store(dtable + (size_t)at * D, D, scale, accumulate);
-            acc.clear();
-            at = BY_ROW ? at + 1 : id;
-          }
-          acc.template add<T>(x[k]);
+      for (int k = 0; k < IN_FLIGHT; k++) r[k] = dout + (size_t)(unsigned)__builtin_amdgcn_readlane(where, min(i + k, m - 1)) * D;
+      typename Piece<E, 1>::template Vec<T> x[IN_FLIGHT][1];
+      acc.load(x, r, D);
+#pragma unroll
+      for (int k = 0; k < IN_FLIGHT; k++) {
+        if (i + k >= m) break;
+        const unsigned id = __builtin_amdgcn_readlane(keys, i + k);
+        while (at != id) {
+          acc.store(dtable + (size_t)at * D, D, scale, accumulate);
+          acc.clear();
+          at = BY_ROW ? at + 1 : id;
         }
+        acc.template add<T>(x[k]);
       }
-      for (; at <= last; at++) {  // (by position: the last id alone)
-        acc.store(dtable + (size_t)at * D, D, scale, accumulate);
-        acc.clear();
-        if (!BY_ROW) break;
-      }
+    }
+    for (; at <= last; at++) {  // (by position: the last id alone)
+      acc.store(dtable + (size_t)at * D, D, scale, accumulate);
+      acc.clear();
+      if (!BY_ROW) break;
     }
     return;
   }
@@ -605,12 +598,10 @@ __global__ __launch_bounds__(256) void embedding_rows_kernel(int N, int V, int D
     const bool beyond = lo + n == base + 64;
     const int hi = beyond ? lo + lower_bound(key + lo, N - lo, v + 1) : lo + n;
     if ((lo + CHUNK - 1) / CHUNK >= hi / CHUNK) {  // (others: a workgroup's)
-      for (int d0 = 0; d0 < D; d0 += Piece<E, STEPS>::WIDTH) {
-        Piece<E, STEPS> acc(d0);
-        if (beyond) add_positions(acc, dout, D, pos, lo, hi);
-        else add_lanes(acc, dout, D, where, lo - base, hi - lo);
-        acc.store(dtable + (size_t)v * D, D, scale, accumulate);
-      }
+      Piece<E, 1> acc(d0);
+      if (beyond) add_positions(acc, dout, D, pos, lo, hi);
+      else add_lanes(acc, dout, D, where, lo - base, hi - lo);
+      acc.store(dtable + (size_t)v * D, D, scale, accumulate);
     }
     lo = hi;
     if (BY_ROW) {
@@ -724,10 +715,14 @@ static int embedding_bwd_t(int N, int V, int D, const int32_t* tokens, const T* 
   const Divider pieces((D + Piece<E, 1>::WIDTH - 1) / Piece<E, 1>::WIDTH);
   hipLaunchKernelGGL((embedding_chunk_kernel<T, E>), wide_grid(((unsigned long long)chunks * pieces.d + 3) / 4), dim3(256), 0, s, N, V, D, pieces, key, pos, dout, sums);
   const bool by_row = !accumulate && !zeros;
-  const int items = ((by_row ? V : N) + ROWS - 1) / ROWS;
-  const dim3 grid = wide_grid(chunks + (items + 3) / 4);
-  if (!by_row) hipLaunchKernelGGL((embedding_rows_kernel<T, E, STEPS, false>), grid, dim3(256), 0, s, N, V, D, chunks, key, pos, dout, sums, scale, accumulate, dtable);
-  else hipLaunchKernelGGL((embedding_rows_kernel<T, E, STEPS, true>), grid, dim3(256), 0, s, N, V, D, chunks, key, pos, dout, sums, scale, 0, dtable);
+  // Rows or positions of a wavefront, us at 768 features by 2, 4, 8 of them:  4000 positions, 50304 rows (by row) 44.6 48.0 50.4;  1000, 8192 (by
+  // row) 18.5 18.4 19.0;  16384, 50304 (by position) 54.6 54.4 55.9;  65536, 50304  85.6 81.3 81.1;  262144, 50304  181 163 158;  200000, 1000  132 120 114
+  const int per = by_row ? (V > 16384 ? 2 : 4) : N > 65536 ? 8 : 4;
+  const unsigned long long items = (((unsigned long long)(by_row ? V : N) + per - 1) / per) * pieces.d;
+  const int chunk_blocks = (int)(chunks * pieces.d);
+  const dim3 grid = wide_grid(chunk_blocks + (items + 3) / 4);
+  if (!by_row) hipLaunchKernelGGL((embedding_rows_kernel<T, E, false>), grid, dim3(256), 0, s, N, V, D, per, chunk_blocks, pieces, key, pos, dout, sums, scale, accumulate, dtable);
+  else hipLaunchKernelGGL((embedding_rows_kernel<T, E, true>), grid, dim3(256), 0, s, N, V, D, per, chunk_blocks, pieces, key, pos, dout, sums, scale, 0, dtable);
   FAX_LAUNCH_CHECK("embedding_bwd");
   return FAX_OK;
 }

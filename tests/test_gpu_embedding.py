@@ -74,6 +74,14 @@ def test_gradient(N, V, D, kind, dtype):
         assert torch.equal(got[untouched], torch.zeros_like(got[untouched]) if before is None else before[untouched])
 
 
+# Several positions to a wavefront, rows in pieces, rows without a position written beside the sort.
+@pytest.mark.parametrize("dtype", ["bf16", "f32"])
+@pytest.mark.parametrize("kind", ["uniform", "padding", "frequent", "none"])
+@pytest.mark.parametrize("N,V,D", [(70000, 900, 20), (66000, 30000, 260), (3000, 20000, 516), (5001, 700, 33), (4500, 66000, 65)])
+def test_gradient_in_pieces(N, V, D, kind, dtype):
+    test_gradient(N, V, D, kind, dtype)
+
+
 def test_gradient_repeats_its_bits_and_leaves_its_workspace_usable():
     gen = torch.Generator().manual_seed(3)
     N, V, D = 30000, 1000, 64
