@@ -42,8 +42,11 @@ typedef __attribute__((ext_vector_type(4))) float f32x4;
 //     {0-3, 8-11} and {4-7, 12-15} (blocks 0+2, 1+3).  Measured: a swizzle that only covers the first
 //     grouping left 31 % of the LDS cycles in bank conflicts (the other kernels' swizzle, made
 //     for 32-row tiles, 47 %); this one leaves none, and the kernel went from 648 K to 580 K clocks.
+// Rows of 128 bytes have half of the banks each, by row parity: the same over eight rows of a parity and eight chunks.
+template <int DH>
 __device__ __forceinline__ int swz16(int row) {
-  const int pair = (row & 3) | ((((row >> 2) ^ (row >> 3)) & 1) << 2);
+  const int mixed = ((row >> 2) ^ (row >> 3)) & 1;
+  const int pair = DH >= 128 ? (row & 3) | (mixed << 2) : ((row >> 1) & 1) | (mixed << 1);
   return (pair << 1) | ((row >> 3) & 1);
 }
 
@@ -56,7 +59,7 @@ __device__ __forceinline__ void tile_dma_seg16(unsigned lds, const bf16_t* __res
   const int lane = threadIdx.x & 63;
   const int seg = wave * (DH / 8 / WAVES) + i;
   const int row = seg * RPI + lane / NCH;
-  const int chunk = (lane % NCH) ^ swz16(row);
+  const int chunk = (lane % NCH) ^ swz16<DH>(row);
   if (!EDGE || (row < rows && chunk < chunks))
     lds_dma16(src, (unsigned)(((size_t)row * ld + chunk * 8) * sizeof(bf16_t)), lds + seg * 1024u);
 }
@@ -65,7 +68,7 @@ __device__ __forceinline__ void tile_dma_seg16(unsigned lds, const bf16_t* __res
 template <int DH>
 __device__ __forceinline__ bf16x8 frag_rows16(const char* lds, int rb, int ks, int lane) {
   const int i = lane & 15, gq = lane >> 4;
-  const unsigned lane_part = i * (DH * 2) + ((gq ^ swz16(i)) << 4);                     // row i, chunk gq
+  const unsigned lane_part = i * (DH * 2) + ((gq ^ swz16<DH>(i)) << 4);                     // row i, chunk gq
   const unsigned off = (lane_part ^ (unsigned)(ks << 6)) + (unsigned)(rb * (DH * 2));  // row rb + i, chunk 4 ks + gq
   return __builtin_bit_cast(bf16x8, *reinterpret_cast<const uint4*>(lds + off));
 }
@@ -79,7 +82,7 @@ __device__ __forceinline__ bf16x8 frag_cols16(const char* lds, int cb, int r0, i
   const int blk = lane >> 4, i = lane & 15;
   const int rl = blk * 4 + (i >> 2);    // row within the group of 16
   const int cl = (i & 3) * 4;           // column within the block of 16
-  const unsigned lane_part = rl * (DH * 2) + (((cl >> 3) ^ swz16(rl)) << 4) + ((cl >> 2) & 1) * 8;
+  const unsigned lane_part = rl * (DH * 2) + (((cl >> 3) ^ swz16<DH>(rl)) << 4) + ((cl >> 2) & 1) * 8;
   const unsigned x = lane_part ^ (unsigned)((cb >> 3) << 4);
   typedef __attribute__((address_space(3))) short4v lds_s4;
   const char* p0 = lds + x + (unsigned)(r0 * (DH * 2));

@@ -32,7 +32,7 @@ struct WindowPlan {
 };
 int window_fwd_mfma(const WindowArgs& a, int waves, int groups, int splits, float* part_o, void* part_ml, hipStream_t s);
 int window_dq_mfma(const WindowArgs& a, int waves, int groups, int splits, float* part_dq, float* part_ds, hipStream_t s);
-int window_dkv_keys(int dh);  // keys of a workgroup
+static constexpr int WINDOW_DKV_KEYS = 64;  // keys of a workgroup
 int window_dkv_mfma(const WindowArgs& a, const WindowPlan& p, float* parts, hipStream_t s);
 int window_fwd_f32(const WindowArgs& a, int splits, float* part_o, void* part_ml, hipStream_t s);
 int window_bwd_f32(const WindowArgs& a, const WindowPlan& p, float* part_dq, float* parts, hipStream_t s);

@@ -229,7 +229,7 @@ static WindowPlan window_plan(const FaxWindowDims& d) {
       p.dq_groups = p.dq_splits == 1 && tiles(seen) >= 6 ? 2 : 1;
     }
     // Keys: those among the sinks are seen by every later query, the others by a window's length of them.
-    p.kv_keys = f32 ? 32 : window_dkv_keys(d.dh);
+    p.kv_keys = f32 ? 32 : WINDOW_DKV_KEYS;
     const long long n = (d.Sk + p.kv_keys - 1) / p.kv_keys, sinks = d.sinks < d.Sk ? d.sinks : d.Sk, all = tiles((long long)d.Sq * group);
     const long long usual = (long long)d.window + p.kv_keys + 64, stream = usual < d.Sq ? tiles(usual * group) : all;
     const double key_bytes = 16.0 * d.dh * p.kv_keys;  // of a tile

@@ -1,20 +1,23 @@
-// Attention in a sliding window with sinks on the CDNA4 matrix cores, bf16: dK and dV (window_mfma.h).  Two forms, as in the full
-// causal attention: up to head width 64 a wave has 32 keys (32x32x16 products), above it 16 (16x16x32), so that two workgroups share a CU.
+// Attention in a sliding window with sinks on the CDNA4 matrix cores, bf16: dK and dV (window_mfma.h).  A wave has 16 keys (16x16x32 products,
+// attn_dkv16.h), so that two workgroups share a CU, three up to head width 64.  (32 keys to a wave read half as much from LDS, but there are fewer, longer
+// workgroups and fewer of them at once; backward pass, us with 32 | 16: 8 x 2048 positions, 12 heads of 64, window 512  188 | 167; the same, all of it
+// 301 | 293; 2 x 4096, 16 heads on 4 of 64, window 1024  181 | 176; 4 x 1000, 12 heads of 48, window 300  46 | 41; 8192, 32 heads on 8 of 128, window
+// 1024, where 32 keys leave one wave to a SIMD  706 | 584.)
 #include "window_mfma.h"
 
 namespace fax {
 
-static constexpr int WPG = 4;  // wavefronts of a workgroup, which share the streamed tiles: a tile for each would leave room for two on a CU
+static constexpr int WPG = WINDOW_DKV_KEYS / 16;  // wavefronts of a workgroup, which share the streamed tiles: a tile for each would leave room for two on a CU
 
-// What both forms have in common: the stream of query tiles and its loads.
-template <int DH, int WAVES, bool SWZ16, bool EDGE>
+// The stream of query tiles and its loads.
+template <int DH, int WAVES, bool EDGE>
 struct QueryStream {
   static constexpr int NSEG = DH / 8 / WAVES, TB = TR * DH * 2, LD_OFF = 2 * TB, STAGE = 2 * TB + 4 * 256;
   const WindowArgs& a;
   int b, hk, wave, lane;
   int i_first, per_head, n;  // first query of a head's first tile; tiles of a head; of all heads
   unsigned sm;
-  TileLoads<DH, WAVES, SWZ16> q, dout;
+  TileLoads<DH, WAVES, true> q, dout;
   bool in_head[NSEG];
   __device__ __forceinline__ QueryStream(const WindowArgs& a_, int b_, int hk_, const QueryRange& r, int wave_, unsigned sm_, int nch)
       : a(a_), q(wave_, a_.sq.row), dout(wave_, a_.sc.row) {
@@ -24,7 +27,7 @@ struct QueryStream {
     per_head = r.i0 < r.i1 ? (r.i1 - i_first + TR - 1) / TR : 0;
     n = per_head * a.group;
 #pragma unroll
-    for (int i = 0; i < NSEG; i++) in_head[i] = !EDGE || lane_in_head<DH, WAVES, SWZ16>(wave, i, nch);
+    for (int i = 0; i < NSEG; i++) in_head[i] = !EDGE || lane_in_head<DH, WAVES, true>(wave, i, nch);
   }
   // Tile t of head g (of the key head's) into buffer `buf`: segments of Q and dO, then lse and delta (lanes 0-15 lse, 16-31 delta, the others the
   // same again).
@@ -46,175 +49,12 @@ struct QueryStream {
 };
 
 // ---------------------------------------------------------------------------------------------
-// 32 keys to a wave.  Per 32-query half: S = Q K^T and dP = dO V^T, P and dS, dV^T += dO^T P and dK^T += Q^T dS.
+// Per 32-query half: S = Q K^T and dP = dO V^T, P and dS, dV^T += dO^T P and dK^T += Q^T dS.
 // ---------------------------------------------------------------------------------------------
 template <int DW, bool EDGE>
-__global__ __launch_bounds__(64 * WPG, 2) void window_dkv_mfma_kernel(WindowArgs a, KeyGrid kg, float* __restrict__ parts) {
+__global__ __launch_bounds__(64 * WPG, DW <= 64 ? 3 : 2) void window_dkv_mfma_kernel(WindowArgs a, KeyGrid kg, float* __restrict__ parts) {
   constexpr int DH = row_width<DW>();
-  typedef QueryStream<DH, WPG, false, EDGE> Stream;
-  constexpr int KS = DW / 16, DT = DW / 32, TB = Stream::TB;
-  constexpr int N = 2 * KS, LEAD = N < 8 ? N : 8;
-  static_assert(N % LEAD == 0 && N > 0, "slot plan");
-  constexpr int RT = 32 * WPG;
-  extern __shared__ __attribute__((aligned(16))) char smem[];
-  const KeyItem it_(kg, a.B * a.Hkv, blockIdx.x, gridDim.x);
-  if (!it_.ok) return;
-  const int b = it_.bh / a.Hkv, hk = it_.bh % a.Hkv;
-  const WindowSeq sq(a, b);
-  const int lane = threadIdx.x & 63, g = lane >> 5;
-  const int wave = __builtin_amdgcn_readfirstlane(threadIdx.x >> 6);
-  const int hw = EDGE ? a.dh : DW, nch = hw / 8;
-  const float scale = a.scale, c = scale * LOG2E;
-  if (EDGE) clear_lds(smem, 2 * Stream::STAGE);
-  const int j0w = it_.tile * RT + wave * 32, jk = j0w + (lane & 31);
-  Stream qs(a, b, hk, QueryRange(a, sq, it_.tile * RT, min((it_.tile + 1) * RT, a.Sk)), wave, lds_addr(smem), nch);
-  const int u0 = (int)((long long)qs.n * it_.split / it_.splits);
-  const int u1 = (int)((long long)qs.n * (it_.split + 1) / it_.splits);
-
-  bf16x8 kf[KS], vf[KS];
-  const bool key_ok = jk < sq.k_len;
-  const bf16_t* kp = strided_row((const bf16_t*)a.k, a.skv, b, min(jk, a.Sk - 1), hk);
-  const bf16_t* vp = strided_row((const bf16_t*)a.v, a.skv, b, min(jk, a.Sk - 1), hk);
-#pragma unroll
-  for (int ks = 0; ks < KS; ks++) {
-    const bool ok = key_ok && (!EDGE || ks * 2 + g < nch);
-    kf[ks] = __builtin_bit_cast(bf16x8, edge_load16(kp + ks * 16 + g * 8, ok));
-    vf[ks] = __builtin_bit_cast(bf16x8, edge_load16(vp + ks * 16 + g * 8, ok));
-  }
-#pragma unroll
-  for (int ks = 0; ks < KS; ks++) { settle(kf[ks]); settle(vf[ks]); }
-  f32x16 dk[DT], dv[DT];
-#pragma unroll
-  for (int dt = 0; dt < DT; dt++)
-#pragma unroll
-    for (int v = 0; v < 16; v++) dk[dt][v] = dv[dt][v] = 0.f;
-  // queries that see this lane's key
-  const QueryRange mine(a, sq, jk, jk + 1);
-  const f32x16 zero = {0.f, 0.f, 0.f, 0.f, 0.f, 0.f, 0.f, 0.f, 0.f, 0.f, 0.f, 0.f, 0.f, 0.f, 0.f, 0.f};
-  auto tile = [&](auto mask_c, int i0, int buf) __attribute__((always_inline)) {
-    constexpr bool MASK = decltype(mask_c)::value;
-    int lane_t = lane;
-    const char* st = smem + buf * Stream::STAGE;
-    auto row_frag = [&](int it, int i) { return frag_rows<DH>(i % 2 ? st + TB : st, it * 32, i / 2, lane_t); };
-    auto col_frag = [&](int it, int i) { return frag_cols<DH>(i % 2 ? st : st + TB, ((i / 2) % DT) * 32, it * 32 + (i / (2 * DT)) * 16, lane_t); };
-    bf16x8 f[LEAD];
-#pragma unroll
-    for (int i = 0; i < LEAD; i++) f[i] = row_frag(0, i);
-    __builtin_amdgcn_sched_barrier(0);
-#pragma unroll
-    for (int it = 0; it < 2; it++) {
-      f32x16 sc, dp;
-      __builtin_amdgcn_s_setprio(1);
-#pragma unroll
-      for (int i = 0; i < N; i++) {
-        if (i % 2 == 0) sc = __builtin_amdgcn_mfma_f32_32x32x16_bf16(f[i % LEAD], kf[i / 2], i < 2 ? zero : sc, 0, 0, 0);
-        else dp = __builtin_amdgcn_mfma_f32_32x32x16_bf16(f[i % LEAD], vf[i / 2], i < 2 ? zero : dp, 0, 0, 0);
-        if (i + LEAD < N) f[i % LEAD] = row_frag(it, i + LEAD);
-        else f[i % LEAD] = col_frag(it, i + LEAD - N);
-        __builtin_amdgcn_sched_barrier(0);
-      }
-      bf16x8 pb[2], db[2];  // P and dS as factors: bf16, half a step off
-      __builtin_amdgcn_s_setprio(0);
-#pragma unroll
-      for (int q = 0; q < 4; q++) {
-        const float4 l4 = Stream::stat4(st, it * 32 + q * 8 + g * 4, 0), d4 = Stream::stat4(st, it * 32 + q * 8 + g * 4, 1);
-#pragma unroll
-        for (int r = 0; r < 4; r++) {
-          const int v = q * 4 + r, i = i0 + it * 32 + q * 8 + g * 4 + r;
-          float e = __builtin_amdgcn_exp2f(fmaf(sc[v], c, -LOG2E * f4_get(l4, r)));
-          float d = e * (dp[v] - f4_get(d4, r));
-          if (MASK) {
-            const bool out = (i < mine.i0) | (i >= mine.i1);
-            e = out ? 0.f : e;
-            d = out ? 0.f : d;
-          }
-          pb[v >> 3][v & 7] = (__bf16)e;
-          db[v >> 3][v & 7] = (__bf16)d;
-        }
-      }
-      __builtin_amdgcn_sched_barrier(0);
-      __builtin_amdgcn_s_setprio(1);
-#pragma unroll
-      for (int i = 0; i < N; i++) {
-        const int hh = i / (2 * DT), dt = (i / 2) % DT;
-        if (i % 2 == 0) dv[dt] = __builtin_amdgcn_mfma_f32_32x32x16_bf16(f[i % LEAD], pb[hh], dv[dt], 0, 0, 0);
-        else dk[dt] = __builtin_amdgcn_mfma_f32_32x32x16_bf16(f[i % LEAD], db[hh], dk[dt], 0, 0, 0);
-        if (i + LEAD < N) f[i % LEAD] = col_frag(it, i + LEAD);
-        else if (it == 0) f[i % LEAD] = row_frag(1, i + LEAD - N);
-        __builtin_amdgcn_sched_barrier(0);
-      }
-    }
-    __builtin_amdgcn_s_setprio(0);
-  };
-
-  if (u0 < u1) {
-    int g_at = u0 / qs.per_head, t = u0 - g_at * qs.per_head;  // head and tile of u
-    qs.load(g_at, t, 0);
-    lds_dma_wait();
-    __syncthreads();
-    // Runs of tiles with and without masks in loops of their own, as in the forward pass.
-    const FullRun full = FullRun::queries(a, sq, j0w, j0w + 32 - 1, qs.i_first);
-    auto any = [&](int t) __attribute__((always_inline)) {
-      const int i0 = qs.i_first + t * TR, p0 = sq.pos0 + i0;
-      return sees_any(a, sq.k_len, p0, p0 + min(TR, a.Sq - i0) - 1, j0w, 32);
-    };
-    auto next = [&](int u) __attribute__((always_inline)) {
-      const bool same = t + 1 < qs.per_head;
-      if (u + 1 < u1) qs.load(same ? g_at : g_at + 1, same ? t + 1 : 0, (u - u0 + 1) & 1);
-    };
-    auto done = [&]() __attribute__((always_inline)) {
-      lds_dma_wait();
-      __syncthreads();
-      if (++t == qs.per_head) { t = 0; g_at++; }
-    };
-    for (int u = u0; u < u1;) {
-      for (; u < u1 && !full.has(t); u++) {
-        next(u);
-        if (any(t)) tile(T_{}, qs.i_first + t * TR, (u - u0) & 1);
-        done();
-      }
-      for (; u < u1 && full.has(t); u++) {
-        next(u);
-        tile(F_{}, qs.i_first + t * TR, (u - u0) & 1);
-        done();
-      }
-    }
-  }
-
-  if (it_.splits > 1) {
-    float* o = parts + kg.part(a, it_.split, it_.bh, jk) * 2 * a.dh;
-#pragma unroll
-    for (int dt = 0; dt < DT; dt++)
-#pragma unroll
-      for (int q = 0; q < 4; q++) {
-        const int d = dt * 32 + q * 8 + g * 4;
-        if (EDGE && dt * 32 + q * 8 >= hw) continue;
-        *reinterpret_cast<float4*>(o + d) = make_float4(dk[dt][q * 4], dk[dt][q * 4 + 1], dk[dt][q * 4 + 2], dk[dt][q * 4 + 3]);
-        *reinterpret_cast<float4*>(o + a.dh + d) = make_float4(dv[dt][q * 4], dv[dt][q * 4 + 1], dv[dt][q * 4 + 2], dv[dt][q * 4 + 3]);
-      }
-    return;
-  }
-  const bool store = jk < a.Sk;
-  const unsigned long long odd = __builtin_amdgcn_ballot_w64(store && not_finite(dv, not_finite(dk, 0.f)) != 0.f);
-  unsigned again = (unsigned)odd | (unsigned)(odd >> 32);
-  if (store && !((again >> (lane & 31)) & 1)) {
-    store_rows<DW, EDGE>(strided_row((bf16_t*)a.dk, a.skv, b, jk, hk), dk, scale, g, hw);
-    store_rows<DW, EDGE>(strided_row((bf16_t*)a.dv, a.skv, b, jk, hk), dv, 1.f, g, hw);
-  }
-  for (; again; again &= again - 1) {
-    int lane_r = lane;
-    settle(lane_r);
-    window_dkv_row<(DW + 63) / 64, bf16_t>(a, b, j0w + __builtin_ctz(again), hk, lane_r);
-  }
-}
-
-// ---------------------------------------------------------------------------------------------
-// 16 keys to a wave (head widths above 64).
-// ---------------------------------------------------------------------------------------------
-template <int DW, bool EDGE>
-__global__ __launch_bounds__(64 * WPG, 2) void window_dkv16_mfma_kernel(WindowArgs a, KeyGrid kg, float* __restrict__ parts) {
-  constexpr int DH = row_width<DW>();
-  typedef QueryStream<DH, WPG, true, EDGE> Stream;
+  typedef QueryStream<DH, WPG, EDGE> Stream;
   constexpr int KS = DW / 32, DT = DW / 16, TB = Stream::TB;
   constexpr int N = 4 * KS, LEAD = N % 8 == 0 ? 8 : 6;
   static_assert(N == 2 * DT && N % LEAD == 0 && N > 0, "slot plan");
@@ -256,7 +96,7 @@ __global__ __launch_bounds__(64 * WPG, 2) void window_dkv16_mfma_kernel(WindowAr
   auto tile = [&](auto mask_c, int i0, int buf) __attribute__((always_inline)) {
     constexpr bool MASK = decltype(mask_c)::value;
     int lane_t = lane;
-    settle(lane_t);  // fragment addresses are formed tile by tile: kept from tile to tile they are some thirty registers
+    if (DW > 64) settle(lane_t);  // fragment addresses are formed tile by tile: kept from tile to tile they are some thirty registers
     const char* st = smem + buf * Stream::STAGE;
     auto row_frag = [&](int it, int i) { return frag_rows16<DH>(i % 2 ? st + TB : st, it * 32 + ((i / 2) / KS) * 16, (i / 2) % KS, lane_t); };
     auto col_frag = [&](int it, int i) { return frag_cols16<DH>(i % 2 ? st : st + TB, (i / 2) * 16, it * 32, lane_t); };
@@ -277,7 +117,7 @@ __global__ __launch_bounds__(64 * WPG, 2) void window_dkv16_mfma_kernel(WindowAr
         else f[i % LEAD] = col_frag(it, i + LEAD - N);
         __builtin_amdgcn_sched_barrier(0);
       }
-      bf16x8 pb, db;
+      bf16x8 pb, db;  // P and dS as factors: bf16, half a step off
       __builtin_amdgcn_s_setprio(0);
 #pragma unroll
       for (int qg = 0; qg < 2; qg++) {
@@ -379,11 +219,9 @@ __global__ __launch_bounds__(64 * WPG, 2) void window_dkv16_mfma_kernel(WindowAr
   for (; again; again &= again - 1) {
     int lane_r = lane;
     settle(lane_r);
-    window_dkv_row<2, bf16_t>(a, b, j0w + __builtin_ctz(again), hk, lane_r);
+    window_dkv_row<(DW + 63) / 64, bf16_t>(a, b, j0w + __builtin_ctz(again), hk, lane_r);
   }
 }
-
-int window_dkv_keys(int dh) { return (dh <= 64 ? 32 : 16) * WPG; }
 
 int window_dkv_mfma(const WindowArgs& a, const WindowPlan& p, float* parts, hipStream_t s) {
   const KeyGrid kg(a, p);
@@ -395,10 +233,10 @@ int window_dkv_mfma(const WindowArgs& a, const WindowPlan& p, float* parts, hipS
     return FAX_OK;
   };
   if (a.dh == 64) return launch(window_dkv_mfma_kernel<64, false>, 64);
-  if (a.dh == 128) return launch(window_dkv16_mfma_kernel<128, false>, 128);
+  if (a.dh == 128) return launch(window_dkv_mfma_kernel<128, false>, 128);
   if (a.dh < 64) return launch(window_dkv_mfma_kernel<64, true>, 64);
-  if (a.dh <= 96) return launch(window_dkv16_mfma_kernel<96, true>, 128);
-  return launch(window_dkv16_mfma_kernel<128, true>, 128);
+  if (a.dh <= 96) return launch(window_dkv_mfma_kernel<96, true>, 128);
+  return launch(window_dkv_mfma_kernel<128, true>, 128);
 }
 
 }  // namespace fax

@@ -31,7 +31,7 @@ struct TileLoads {
   unsigned off[OFFS];
   int wave, ld;
   __device__ __forceinline__ static int chunk_of(int row) {
-    return ((threadIdx.x & 63) % NCH) ^ (SWZ16 ? swz16(row) : swz<DH>(row));
+    return ((threadIdx.x & 63) % NCH) ^ (SWZ16 ? swz16<DH>(row) : swz<DH>(row));
   }
   __device__ __forceinline__ TileLoads(int wave_, long long ld_) {
     wave = wave_;
@@ -77,7 +77,7 @@ __device__ __forceinline__ bool lane_in_head(int wave, int i, int chunks) {
   constexpr int NCH = DH / 8, RPI = 64 / NCH, NSEG = DH / 8 / WAVES;
   const int lane = threadIdx.x & 63;
   const int row = (wave * NSEG + i) * RPI + lane / NCH;
-  return ((lane % NCH) ^ (SWZ16 ? swz16(row) : swz<DH>(row))) < chunks;
+  return ((lane % NCH) ^ (SWZ16 ? swz16<DH>(row) : swz<DH>(row))) < chunks;
 }
 
 // x and y as bf16 pairs: elements 2 n and 2 n + 1 of hi cut off (not rounded), of lo what that leaves, rounded: 2^-16 off each instead of 2^-8.
