@@ -173,7 +173,7 @@ static bool strides_fit(const FaxStrides& s, int unit) { return s.batch % unit =
 
 // Into how many parts a stream of `tiles` tiles is cut, with `blocks` workgroups: by an estimate in us.  tile: of a tile, part_tile: of a tile
 // in a cut stream; at_once: workgroups that the chip works on side by side without slowing each other down; part_bytes: what a part writes and the joining
-// kernel reads.  6 us: the second kernel.
+// kernel reads.  6 us and 0.04 to a part: the second kernel.
 struct StreamCost { double tile, part_tile, at_once; bool whole_rounds; };
 static int cut_stream(double blocks, long long tiles, const StreamCost& c, double part_bytes) {
   int best = 1;
@@ -182,23 +182,23 @@ static int cut_stream(double blocks, long long tiles, const StreamCost& c, doubl
     double rounds = blocks * n / c.at_once;
     if (rounds < 1.0) rounds = 1.0;
     else if (c.whole_rounds) rounds = ceil(rounds);
-    const double us = 6.0 + (double)((tiles + n - 1) / n) * c.part_tile * rounds + part_bytes * n / 2.5e6;
+    const double us = 6.0 + 0.04 * n + (double)((tiles + n - 1) / n) * c.part_tile * rounds + part_bytes * n / 2.5e6;
     if (us < 0.97 * least) { least = us; best = n; }
   }
   return best;
 }
 
-// Measured, back to back in a graph, us by parts (bf16, heads on key heads x width, window):
-//   forward  512 queries over 2048 keys, 8 on 8 x 128, 2048 (32 workgroups, 34 tiles)   1: 49  4: 29  8: 27  16: 29;  16 on 4 over 8192 (64)  52  37  35  44;
-//            two of that (128) 53  47  56;  three (192) 54  2: 68;  16 on 4 x 64, 1024 (64, 18 tiles) 23  21  25;  1024 of 16 x 64, 300 (128, 7 tiles) 14.5  2: 24
-//            tokens over 4096 keys, 32 on 8 x 128: one (8 workgroups) 149  4: 54  8: 30  16: 19  32: 13  64: 12;  four 150  55  32  22  26;  sixteen 150  57  61  68
-//   dQ       4096 of 2 on 1 x 128, all (64, up to 64 tiles), of both kernels 363  2: 302  4: 272  8: 269  16: 282;  1024 of 16 x 64, 300 38  2: 43
-//   dK, dV   the same two 363  262  212  192  201;  38  45  49
+// Measured, back to back in a graph, us by parts (bf16, heads on key heads x width, window; where there is one part, two groups where the rule has them):
+//   forward  512 queries over 2048 keys, 8 on 8 x 128, 2048 (32 workgroups, 34 tiles)  1: 36  4: 28  8: 28  16: 30;  16 on 4 over 8192 (64)  37  37  36  47;
+//            two of that (128)  38  4: 47  8: 56;  three (192)  40  2: 67;  16 on 4 x 64, 1024 (64, 18 tiles)  18  2: 29;  1024 of 16 x 64, 300 (128, 7)  13  24
+//            tokens over 4096 keys, 32 on 8 x 128: one (8 workgroups)  79  4: 32  8: 20  16: 14  32: 11.7  64: 12.8;  four  81  34  23  21  25;  sixteen  82  52  51  55
+//   backward, by parts of dQ's streams  4096 of 2 on 1 x 128, all (64 workgroups, up to 64 tiles)  146  2: 124  4: 99  8: 98  16: 110;  1024 of 16 x 64, 300  27  34  39
+//             by those of dK and dV     the same two  231  151  110  99  111;  28  41  47
 // and by groups of wavefronts, us with one | with two (forward; backward, where only dQ has them):
-//   512 queries over 8192 keys, 16 on 4 x 128, 2048, of two (128 workgroups)  46.9 | 37.2; of four (256)  50.1 | 43.9;  four, x 64, 1024  21.2 | 18.4
-//   1024 of 16 x 64, 300 (128, 7 tiles)  12.9 | 11.8; 34.4 | 34.1    1000 of 15 on 5 x 80, 300 (120)  16.5 | 14.1; 47.4 | 45.0
-//   2048 of 16 x 64, 512 (256, 10 tiles)  16.5 | 14.5; 55.1 | 53.7   eight of 256 of 16 x 128, all (256, 4 tiles)  13.5 | 13.4; 37.7 | 39.8
-//   eight of 128 of 16 x 128, all (128, 2 tiles)  9.9 | 10.4; 23.4 | 25.5
+//   512 queries over 8192 keys, 16 on 4 x 128, 2048, of two (128 workgroups)  49.8 | 39.9; of four (256)  53.3 | 45.5;  four, x 64, 1024  22.5 | 19.6
+//   1024 of 16 x 64, 300 (128, 7 tiles)  13.9 | 12.7; 28.2 | 27.8    1000 of 15 on 5 x 80, 300 (120)  17.7 | 15.3; 49.2 | 45.9
+//   2048 of 16 x 64, 512 (256, 10 tiles)  17.8 | 15.9; 46.1 | 44.8   eight of 256 of 16 x 128, all (256, 4 tiles)  14.4 | 14.5; 39.2 | 40.9
+//   eight of 128 of 16 x 128, all (128, 2 tiles)  11.0 | 11.3; 24.3 | 26.3
 static WindowPlan window_plan(const FaxWindowDims& d) {
   WindowPlan p = {};
   p.form = FAX_ATTENTION_SCALAR;
@@ -217,7 +217,7 @@ static WindowPlan window_plan(const FaxWindowDims& d) {
     const bool alone = !f32 && p.waves == 1;  // a wavefront with tiles of its own: its workgroups are two to a CU
     const int unit_keys = f32 ? 128 : 64;
     const double w = d.dh / 128.0;
-    const StreamCost fwd = f32 ? StreamCost{1 + 3.4 * w, 1 + 3.4 * w, 256, false} : alone ? StreamCost{2.3, 2.3, 512, true} : StreamCost{1.35, 1.7, 384, false};
+    const StreamCost fwd = f32 ? StreamCost{1 + 3.4 * w, 1 + 3.4 * w, 256, false} : alone ? StreamCost{1.25, 1.25, 512, true} : StreamCost{1.35, 1.7, 384, false};
     const StreamCost dq = f32 ? StreamCost{1 + 5.1 * w, 1 + 5.1 * w, 256, false} : alone ? StreamCost{3.0, 3.0, 512, true} : StreamCost{2.0, 2.0, 384, false};
     const StreamCost dkv = f32 ? StreamCost{1 + 6.8 * w, 1 + 6.8 * w, 256, false} : StreamCost{2.0, 2.0, 400, false};
     auto tiles = [&](long long keys) { return (keys + unit_keys - 1) / unit_keys; };
