@@ -1,4 +1,8 @@
 // Embedding lookup with scaling, and its gradient by sorted tokens.  Both are bound by memory.
+// Measured at 65536 positions, table of 50304 x 768, frequencies like a text's: lookup (bf16) 22.5 us, 178 MB at 7.9 TB/s (frequent rows come out of the
+// caches); gradient (bf16 upstream, fp32 table, 255 MB that have to move: 51 us at the rate of a large copy) 79 us: sorting 34 us, of which the zeros of
+// rows without a position, 104 MB, fill 24; the chunks' sums 13 us, the other rows 34 us.  The sort's launches depend on each other, so some 10 us
+// of the 34 have the chip idle.
 #include <type_traits>
 
 #include "fax_internal.h"

@@ -2,6 +2,8 @@
 // fp32 (attn_f32_common.h).  A workgroup owns 32 rows of a key head (forward, dQ; row r is query r / group, query head r % group) or 32
 // keys (dK, dV); its four wavefronts take the 32-row tiles of the other index that are seen in turn, and their results are added through LDS in wave
 // order.  Long streams (single tokens over a cache; the sinks' keys, which every later query sees) are cut over workgroups and joined.
+// Bound by the matrix instruction (154 TFLOP/s for a large fp32 product) where streams are long: 2 x 2048 positions, 16 heads on 4 of 128, window 512,
+// sinks 4: forward 185 us (82 TFLOP/s), backward 686 us (55; seven products are formed for five); 4 x 1024, 8 heads of 64, window 256: 44 and 125 us.
 #include "attn_f32_common.h"
 #include "window_tiles.h"
 
