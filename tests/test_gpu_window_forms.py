@@ -1,5 +1,7 @@
 """fax_window_attention_*: every form that its sizes can take, each at a size that takes it (fax_window_attention_route says so), against
 float64 with derived bounds."""
+import math
+
 import pytest
 import torch
 
@@ -60,6 +62,29 @@ def test_two_groups(B, S, H, Hkv, window, sinks, dq, dh):
     k_len = (S - 37 * short).clamp(min=1)
     k_len[-1] = 50 if B > 3 else 0
     both(B, S, S, H, Hkv, dh, "bf16", window, sinks, 3 * short, k_len)
+
+
+@pytest.mark.parametrize("dh", [64, 80, 128])
+def test_two_groups_at_their_edges(dh):
+    """Large scores; what no query sees is not used, whatever it holds; a NaN reaches the queries that see it, through whichever group's tiles."""
+    B, S, H, window, sinks = 4, 700, 8, 400, 2
+    r = route(B, S, S, H, H, dh, "bf16", window, sinks)
+    assert (r.fwd_groups, r.dq_groups, r.fwd_splits, r.dq_splits) == (2, 2, 1, 1), forms(r)
+    both(B, S, S, H, H, dh, "bf16", window, sinks, sharp=40.0)
+    q, k, v, d = make(B, S, S, H, H, dh, "bf16")
+    q_pos, k_len = torch.zeros(B, dtype=torch.int32), torch.tensor([700, 300, 90, 0], dtype=torch.int32)
+    ref = orc.window_attention(q.double(), k.double(), v.double(), window, sinks, q_pos, k_len, d.double(), TD["bf16"])
+    for b in range(B):
+        k[b, k_len[b]:], v[b, k_len[b]:] = math.inf, math.nan
+    check(run(*(t.to(DEV) for t in (q, k, v, d)), window, sinks, q_pos, k_len), ref)
+    for at in (70, 150):
+        k[0], v[0] = 1.0, 1.0
+        v[0, at] = math.nan
+        got = run(*(t.to(DEV) for t in (q, k, v, d)), window, sinks, q_pos, k_len)
+        see = orc.window_mask(S, S, window, sinks, q_pos.long(), k_len.long())[0][:, at]
+        for name in ("ctx", "dq"):
+            assert torch.equal(torch.isnan(got[name][0]).any(-1).any(-1), see), name
+        assert torch.isfinite(got["ctx"][1:]).all()
 
 
 @pytest.mark.parametrize("dtype", ["bf16", "f32"])
