@@ -167,7 +167,7 @@ __device__ __forceinline__ void settle(T& v) { asm volatile("" : "+v"(v)); }
 // that had to be NaN is NaN again, one that did not is what those kernels give.  The check is an FMA
 // per accumulator register and pass, about 1 % of the shortest pass's vector work; the second
 // computation costs what the scalar kernels cost, for those rows alone.
-template <int DW> constexpr int row_width() { return DW <= 64 ? 64 : 128; }
+template <int DW> constexpr int row_width() { return DW <= 64 ? 64 : DW <= 128 ? 128 : 256; }
 __device__ __forceinline__ uint4 edge_load16(const bf16_t* p, bool ok) {
   return ok ? *reinterpret_cast<const uint4*>(p) : make_uint4(0u, 0u, 0u, 0u);
 }

@@ -58,7 +58,7 @@ static WindowArgs window_args(const FaxWindowDims& d) {
 // Joins the parts that the workgroups of a cut row left, their sums undivided, with their reference points and denominators: one wavefront to a
 // row.  octaves: of the reference points' unit; unit: of it in scaled scores.  What one wavefront loads at once are all parts' points and up to eight
 // parts' sums.
-template <typename T>
+template <int R, typename T>  // R: 64-wide pieces of a head
 __global__ __launch_bounds__(256) void window_join_kernel(WindowArgs a, int splits, const float* __restrict__ part_o, const float2* __restrict__ part_ml,
                                                           float octaves, float unit) {
   const long long row = (long long)blockIdx.x * 4 + (threadIdx.x >> 6), rows = (long long)a.B * a.Hkv * a.Sq * a.group;
@@ -73,32 +73,34 @@ __global__ __launch_bounds__(256) void window_join_kernel(WindowArgs a, int spli
   const float2 mine = lane < splits ? ml[lane] : make_float2(-3.4028235e38f, 0.f);
   const float M = wave_max(mine.x), weight = __builtin_amdgcn_exp2f((mine.x - M) * octaves);
   const float L = wave_sum(mine.y * weight);
-  float acc[2] = {0.f, 0.f};
-  const int d0 = min(lane, a.dh - 1), d1 = min(lane + 64, a.dh - 1);
+  float acc[R] = {};
   for (int s0 = 0; s0 < splits; s0 += 8) {  // (beyond the last part: loads of the last)
-    float x[8][2];
+    float x[8][R];
 #pragma unroll
     for (int k = 0; k < 8; k++) {
       const float* p = o + (long long)min(s0 + k, splits - 1) * a.dh;
-      x[k][0] = p[d0];
-      x[k][1] = p[d1];
+#pragma unroll
+      for (int c = 0; c < R; c++) x[k][c] = p[min(lane + 64 * c, a.dh - 1)];
     }
 #pragma unroll
     for (int k = 0; k < 8; k++) {
       const float w = __uint_as_float(__builtin_amdgcn_readlane(__float_as_uint(weight), s0 + k));
-      acc[0] = s0 + k < splits ? fmaf(x[k][0], w, acc[0]) : acc[0];
-      acc[1] = s0 + k < splits ? fmaf(x[k][1], w, acc[1]) : acc[1];
+#pragma unroll
+      for (int c = 0; c < R; c++) acc[c] = s0 + k < splits ? fmaf(x[k][c], w, acc[c]) : acc[c];
     }
   }
-  if (__any(!(fabsf(acc[0]) <= 3.4028235e38f) || !(fabsf(acc[1]) <= 3.4028235e38f)) || !(L <= 3.4028235e38f)) {
-    window_fwd_row<2, T>(a, b, i, h, lane);
+  bool odd = !(L <= 3.4028235e38f);
+#pragma unroll
+  for (int c = 0; c < R; c++) odd |= !(fabsf(acc[c]) <= 3.4028235e38f);
+  if (__any(odd)) {
+    window_fwd_row<R, T>(a, b, i, h, lane);
     return;
   }
   const bool none = L == 0.f;
   const float inv = none ? 0.f : 1.f / L;
   T* out = strided_row((T*)a.ctx, a.sc, b, i, h);
 #pragma unroll
-  for (int k = 0; k < 2; k++) {
+  for (int k = 0; k < R; k++) {
     const int d = lane + 64 * k;
     if (d < a.dh) out[d] = from_f<T>(acc[k] * inv);
   }
@@ -106,7 +108,7 @@ __global__ __launch_bounds__(256) void window_join_kernel(WindowArgs a, int spli
 }
 
 // dQ of cut rows: the parts added in order, one wavefront to a row.  part_ds: the parts of delta (NULL: it is there already).
-template <typename T>
+template <int R, typename T>
 __global__ __launch_bounds__(256) void window_fold_dq_kernel(WindowArgs a, int splits, const float* __restrict__ part_dq, const float* __restrict__ part_ds) {
   const long long row = (long long)blockIdx.x * 4 + (threadIdx.x >> 6), rows = (long long)a.B * a.Hkv * a.Sq * a.group;
   if (row >= rows) return;
@@ -119,28 +121,28 @@ __global__ __launch_bounds__(256) void window_fold_dq_kernel(WindowArgs a, int s
     const float delta = wave_sum(lane < splits ? part_ds[row * splits + lane] : 0.f);
     if (lane == 0) a.delta[((long long)b * a.H + h) * a.Sq + i] = delta;
   }
-  float acc[2] = {0.f, 0.f};
-  const int d0 = min(lane, a.dh - 1), d1 = min(lane + 64, a.dh - 1);
+  float acc[R] = {}, odd = 0.f;
 #pragma unroll 8
-  for (int s = 0; s < splits; s++) {
-    acc[0] += o[(long long)s * a.dh + d0];
-    acc[1] += o[(long long)s * a.dh + d1];
-  }
-  if (sizeof(T) == 2 && __any(acc[0] * 0.f + acc[1] * 0.f != 0.f)) {  // (the fp32 kernels keep masked rows out of their sums)
+  for (int s = 0; s < splits; s++)
+#pragma unroll
+    for (int c = 0; c < R; c++) acc[c] += o[(long long)s * a.dh + min(lane + 64 * c, a.dh - 1)];
+#pragma unroll
+  for (int c = 0; c < R; c++) odd = fmaf(acc[c], 0.f, odd);
+  if (sizeof(T) == 2 && __any(odd != 0.f)) {  // (the fp32 kernels keep masked rows out of their sums)
     __threadfence();
-    window_dq_row<2, T>(a, b, i, h, lane);
+    window_dq_row<R, T>(a, b, i, h, lane);
     return;
   }
   T* out = strided_row((T*)a.dq, a.sq, b, i, h);
 #pragma unroll
-  for (int k = 0; k < 2; k++) {
+  for (int k = 0; k < R; k++) {
     const int d = lane + 64 * k;
     if (d < a.dh) out[d] = from_f<T>(acc[k] * a.scale);
   }
 }
 
 // The parts of the cut tiles' keys, added in order: one wavefront to a key.
-template <typename T>
+template <int R, typename T>
 __global__ __launch_bounds__(256) void window_fold_kernel(WindowArgs a, KeyGrid kg, const float* __restrict__ parts) {
   const int from = kg.fold_from(), n = kg.fold_keys(a);
   const long long item = (long long)blockIdx.x * 4 + (threadIdx.x >> 6);
@@ -148,29 +150,31 @@ __global__ __launch_bounds__(256) void window_fold_kernel(WindowArgs a, KeyGrid 
   if (item >= (long long)n * a.B * a.Hkv) return;
   const int j = from + (int)(item % n), bh = (int)(item / n);
   const int splits = j < kg.sink_tiles * kg.keys ? kg.sink_splits : kg.rest_splits;
-  float s[4] = {0.f, 0.f, 0.f, 0.f};  // dK and dV, two 64-wide pieces each
-  const int d0 = min(lane, a.dh - 1), d1 = min(lane + 64, a.dh - 1);
+  float dk[R] = {}, dv[R] = {}, odd = 0.f;
 #pragma unroll 4
   for (int p = 0; p < splits; p++) {
     const float* o = parts + kg.part(a, p, bh, j) * 2 * a.dh;
-    s[0] += o[d0];
-    s[1] += o[d1];
-    s[2] += o[a.dh + d0];
-    s[3] += o[a.dh + d1];
+#pragma unroll
+    for (int c = 0; c < R; c++) {
+      dk[c] += o[min(lane + 64 * c, a.dh - 1)];
+      dv[c] += o[a.dh + min(lane + 64 * c, a.dh - 1)];
+    }
   }
+#pragma unroll
+  for (int c = 0; c < R; c++) odd = fmaf(dk[c], 0.f, fmaf(dv[c], 0.f, odd));
   const int b = bh / a.Hkv, hk = bh % a.Hkv;
-  if (__any((s[0] * 0.f + s[1] * 0.f) + (s[2] * 0.f + s[3] * 0.f) != 0.f)) {
-    window_dkv_row<2, T>(a, b, j, hk, lane);
+  if (__any(odd != 0.f)) {
+    window_dkv_row<R, T>(a, b, j, hk, lane);
     return;
   }
   T* ko = strided_row((T*)a.dk, a.skv, b, j, hk);
   T* vo = strided_row((T*)a.dv, a.skv, b, j, hk);
 #pragma unroll
-  for (int k = 0; k < 2; k++) {
+  for (int k = 0; k < R; k++) {
     const int d = lane + 64 * k;
     if (d < a.dh) {
-      ko[d] = from_f<T>(s[k] * a.scale);
-      vo[d] = from_f<T>(s[2 + k]);
+      ko[d] = from_f<T>(dk[k] * a.scale);
+      vo[d] = from_f<T>(dv[k]);
     }
   }
 }
@@ -213,7 +217,7 @@ static WindowPlan window_plan(const FaxWindowDims& d) {
   p.fwd_groups = p.dq_groups = p.fwd_splits = p.dq_splits = p.sink_splits = p.rest_splits = 1;
   const int unit = d.dtype == FAX_F32 ? 4 : 8, group = d.H / d.Hkv;
   const long long heads = (long long)d.B * d.Hkv, rows = (long long)d.Sq * group;
-  if (d.dh % unit == 0 && d.dh <= 128 && strides_fit(d.q, unit) && strides_fit(d.kv, unit) && strides_fit(d.ctx, unit) && rows < (1 << 30)) {
+  if (d.dh % unit == 0 && d.dh <= (d.dtype == FAX_F32 ? 128 : 256) && strides_fit(d.q, unit) && strides_fit(d.kv, unit) && strides_fit(d.ctx, unit) && rows < (1 << 30)) {
     const bool f32 = d.dtype == FAX_F32;
     p.form = f32 ? FAX_ATTENTION_F32 : d.dh == 64 || d.dh == 128 ? FAX_ATTENTION_MFMA : FAX_ATTENTION_EDGE;
     p.waves = !f32 && rows > 32 ? 4 : 1;
@@ -224,14 +228,15 @@ static WindowPlan window_plan(const FaxWindowDims& d) {
     const bool alone = !f32 && p.waves == 1;  // a wavefront with tiles of its own: its workgroups are two to a CU
     const int unit_keys = f32 ? 128 : 64;
     const double w = d.dh / 128.0;
-    const StreamCost fwd = f32 ? StreamCost{1 + 3.4 * w, 1 + 3.4 * w, 256, false} : alone ? StreamCost{1.25, 1.25, 512, true} : StreamCost{1.35, 1.7, 384, false};
-    const StreamCost dq = f32 ? StreamCost{1 + 5.1 * w, 1 + 5.1 * w, 256, false} : alone ? StreamCost{3.0, 3.0, 512, true} : StreamCost{2.0, 2.0, 384, false};
-    const StreamCost dkv = f32 ? StreamCost{1 + 6.8 * w, 1 + 6.8 * w, 256, false} : StreamCost{2.0, 2.0, 400, false};
+    const bool wide = d.dh > 128;  // bf16: one workgroup to a CU, tiles twice as wide
+    const StreamCost fwd = f32 ? StreamCost{1 + 3.4 * w, 1 + 3.4 * w, 256, false} : wide ? StreamCost{3.0, 3.5, 256, alone} : alone ? StreamCost{1.25, 1.25, 512, true} : StreamCost{1.35, 1.7, 384, false};
+    const StreamCost dq = f32 ? StreamCost{1 + 5.1 * w, 1 + 5.1 * w, 256, false} : wide ? StreamCost{7.0, 7.0, 256, alone} : alone ? StreamCost{3.0, 3.0, 512, true} : StreamCost{2.0, 2.0, 384, false};
+    const StreamCost dkv = f32 ? StreamCost{1 + 6.8 * w, 1 + 6.8 * w, 256, false} : wide ? StreamCost{5.0, 5.0, 256, false} : StreamCost{2.0, 2.0, 400, false};
     auto tiles = [&](long long keys) { return (keys + unit_keys - 1) / unit_keys; };
     p.fwd_splits = cut_stream(blocks, tiles(seen), fwd, row_bytes);
     p.dq_splits = cut_stream(blocks, tiles(seen), dq, row_bytes);
     // Two groups of wavefronts to a workgroup where there is one to a CU: one group's tiles do not fill it, and adding up takes a microsecond or two.
-    if (p.waves == 4 && blocks <= 256) {
+    if (p.waves == 4 && blocks <= 256 && !wide) {
       p.fwd_groups = p.fwd_splits == 1 && tiles(seen) >= 4 ? 2 : 1;
       p.dq_groups = p.dq_splits == 1 && tiles(seen) >= 6 ? 2 : 1;
     }
@@ -319,8 +324,11 @@ int window_fwd(const FaxWindowDims& d, const void* q, const void* k, const void*
     if (p.fwd_splits > 1) {
       const float log2e = 1.4426950408889634f;
       const dim3 grid((unsigned)(((long long)a.B * a.H * a.Sq + 3) / 4));
-      if (d.dtype == FAX_F32) hipLaunchKernelGGL(window_join_kernel<float>, grid, dim3(256), 0, s, a, p.fwd_splits, part_o, part_ml, log2e, 1.f);
-      else hipLaunchKernelGGL(window_join_kernel<bf16_t>, grid, dim3(256), 0, s, a, p.fwd_splits, part_o, part_ml, a.scale * log2e, a.scale);
+      if (d.dtype == FAX_F32) hipLaunchKernelGGL((window_join_kernel<2, float>), grid, dim3(256), 0, s, a, p.fwd_splits, part_o, part_ml, log2e, 1.f);
+      else {
+        if (d.dh <= 128) hipLaunchKernelGGL((window_join_kernel<2, bf16_t>), grid, dim3(256), 0, s, a, p.fwd_splits, part_o, part_ml, a.scale * log2e, a.scale);
+        else hipLaunchKernelGGL((window_join_kernel<4, bf16_t>), grid, dim3(256), 0, s, a, p.fwd_splits, part_o, part_ml, a.scale * log2e, a.scale);
+      }
     }
   }
   FAX_LAUNCH_CHECK("window_attention_fwd");
@@ -345,18 +353,24 @@ int window_bwd(const FaxWindowDims& d, const void* q, const void* k, const void*
     if (p.form == FAX_ATTENTION_F32) {
       FAX_TRY(rows_launch<3>(a, d.dtype, s));
       FAX_TRY(window_bwd_f32(a, p, part_dq, parts, s));
-      if (p.dq_splits > 1) hipLaunchKernelGGL(window_fold_dq_kernel<float>, dim3(row_blocks), dim3(256), 0, s, a, p.dq_splits, part_dq, (const float*)nullptr);
+      if (p.dq_splits > 1) hipLaunchKernelGGL((window_fold_dq_kernel<2, float>), dim3(row_blocks), dim3(256), 0, s, a, p.dq_splits, part_dq, (const float*)nullptr);
     } else {
       // dQ first: it also leaves delta, which dK and dV need
       FAX_TRY(window_dq_mfma(a, p.waves, p.dq_groups, p.dq_splits, part_dq, part_ds, s));
-      if (p.dq_splits > 1) hipLaunchKernelGGL(window_fold_dq_kernel<bf16_t>, dim3(row_blocks), dim3(256), 0, s, a, p.dq_splits, part_dq, part_ds);
+      if (p.dq_splits > 1) {
+        if (d.dh <= 128) hipLaunchKernelGGL((window_fold_dq_kernel<2, bf16_t>), dim3(row_blocks), dim3(256), 0, s, a, p.dq_splits, part_dq, part_ds);
+        else hipLaunchKernelGGL((window_fold_dq_kernel<4, bf16_t>), dim3(row_blocks), dim3(256), 0, s, a, p.dq_splits, part_dq, part_ds);
+      }
       FAX_TRY(window_dkv_mfma(a, p, parts, s));
     }
     if (p.sink_splits > 1 || p.rest_splits > 1) {
       const KeyGrid kg(a, p);
       const dim3 grid((unsigned)(((long long)kg.fold_keys(a) * a.B * a.Hkv + 3) / 4));
-      if (d.dtype == FAX_F32) hipLaunchKernelGGL(window_fold_kernel<float>, grid, dim3(256), 0, s, a, kg, parts);
-      else hipLaunchKernelGGL(window_fold_kernel<bf16_t>, grid, dim3(256), 0, s, a, kg, parts);
+      if (d.dtype == FAX_F32) hipLaunchKernelGGL((window_fold_kernel<2, float>), grid, dim3(256), 0, s, a, kg, parts);
+      else {
+        if (d.dh <= 128) hipLaunchKernelGGL((window_fold_kernel<2, bf16_t>), grid, dim3(256), 0, s, a, kg, parts);
+        else hipLaunchKernelGGL((window_fold_kernel<4, bf16_t>), grid, dim3(256), 0, s, a, kg, parts);
+      }
     }
   }
   FAX_LAUNCH_CHECK("window_attention_bwd");

@@ -52,7 +52,7 @@ struct QueryStream {
 // Per 32-query half: S = Q K^T and dP = dO V^T, P and dS, dV^T += dO^T P and dK^T += Q^T dS.
 // ---------------------------------------------------------------------------------------------
 template <int DW, bool EDGE>
-__global__ __launch_bounds__(64 * WPG, DW <= 64 ? 3 : 2) void window_dkv_mfma_kernel(WindowArgs a, KeyGrid kg, float* __restrict__ parts) {
+__global__ __launch_bounds__(64 * WPG, DW <= 64 ? 3 : DW <= 128 ? 2 : 1) void window_dkv_mfma_kernel(WindowArgs a, KeyGrid kg, float* __restrict__ parts) {
   constexpr int DH = row_width<DW>();
   typedef QueryStream<DH, WPG, EDGE> Stream;
   constexpr int KS = DW / 32, DT = DW / 16, TB = Stream::TB;
@@ -236,7 +236,8 @@ int window_dkv_mfma(const WindowArgs& a, const WindowPlan& p, float* parts, hipS
   if (a.dh == 128) return launch(window_dkv_mfma_kernel<128, false>, 128);
   if (a.dh < 64) return launch(window_dkv_mfma_kernel<64, true>, 64);
   if (a.dh <= 96) return launch(window_dkv_mfma_kernel<96, true>, 128);
-  return launch(window_dkv_mfma_kernel<128, true>, 128);
+  if (a.dh < 128) return launch(window_dkv_mfma_kernel<128, true>, 128);
+  return launch(window_dkv_mfma_kernel<256, true>, 256);
 }
 
 }  // namespace fax

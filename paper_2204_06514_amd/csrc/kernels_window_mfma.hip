@@ -10,7 +10,7 @@ namespace fax {
 // unscaled score) and their denominators, for window_join_kernel.
 // ---------------------------------------------------------------------------------------------
 template <int DW, bool EDGE, int G, int WPG, bool PART>
-__global__ __launch_bounds__(64 * G * WPG, 2) void window_fwd_mfma_kernel(WindowArgs a, int n_tiles, int items, int splits, float* __restrict__ part_o,
+__global__ __launch_bounds__(64 * G * WPG, DW > 128 ? 1 : 2) void window_fwd_mfma_kernel(WindowArgs a, int n_tiles, int items, int splits, float* __restrict__ part_o,
                                                                       float2* __restrict__ part_ml) {
   constexpr int DH = row_width<DW>();  // row length in LDS
   constexpr int KS = DW / 16, DT = DW / 32, TB = TR * DH * 2;
@@ -232,7 +232,7 @@ __global__ __launch_bounds__(64 * G * WPG, 2) void window_fwd_mfma_kernel(Window
 // dQ, and delta = dctx . ctx by row.  The same tiles; per 32-key half S^T = K Q^T and dP^T = V dO^T, dS^T = P^T (dP^T - delta), dQ^T += K^T dS^T.
 // ---------------------------------------------------------------------------------------------
 template <int DW, bool EDGE, int G, int WPG, bool PART>
-__global__ __launch_bounds__(64 * G * WPG, 2) void window_dq_mfma_kernel(WindowArgs a, int n_tiles, int items, int splits, float* __restrict__ part_dq,
+__global__ __launch_bounds__(64 * G * WPG, DW > 128 ? 1 : 2) void window_dq_mfma_kernel(WindowArgs a, int n_tiles, int items, int splits, float* __restrict__ part_dq,
                                                                      float* __restrict__ part_ds) {
   constexpr int DH = row_width<DW>();
   constexpr int KS = DW / 16, DT = DW / 32, TB = TR * DH * 2;
@@ -434,7 +434,7 @@ template <typename F>
 static int by_width(int dh, F f) {
   if (dh == 64) return f(I<64>{}, F_{});
   if (dh == 128) return f(I<128>{}, F_{});
-  return dh < 64 ? f(I<64>{}, T_{}) : dh <= 96 ? f(I<96>{}, T_{}) : f(I<128>{}, T_{});
+  return dh < 64 ? f(I<64>{}, T_{}) : dh <= 96 ? f(I<96>{}, T_{}) : dh < 128 ? f(I<128>{}, T_{}) : f(I<256>{}, T_{});
 }
 
 int window_fwd_mfma(const WindowArgs& a, int waves, int groups, int splits, float* part_o, void* part_ml, hipStream_t s) {
@@ -450,7 +450,8 @@ int window_fwd_mfma(const WindowArgs& a, int waves, int groups, int splits, floa
       hipLaunchKernelGGL(kern, dim3(xcd_grid(items)), dim3(64 * groups * waves), lds, s, a, n_tiles, (int)items, splits, part_o, (float2*)part_ml);
       return FAX_OK;
     };
-    if (groups > 1) return go(I<2>{}, I<4>{}, F_{});
+    if constexpr (DW <= 128)
+      if (groups > 1) return go(I<2>{}, I<4>{}, F_{});
     if (splits > 1) return waves == 1 ? go(I<1>{}, I<1>{}, T_{}) : go(I<1>{}, I<4>{}, T_{});
     return waves == 1 ? go(I<1>{}, I<1>{}, F_{}) : go(I<1>{}, I<4>{}, F_{});
   });
@@ -469,7 +470,8 @@ int window_dq_mfma(const WindowArgs& a, int waves, int groups, int splits, float
       hipLaunchKernelGGL(kern, dim3(xcd_grid(items)), dim3(64 * groups * waves), lds, s, a, n_tiles, (int)items, splits, part_dq, part_ds);
       return FAX_OK;
     };
-    if (groups > 1) return go(I<2>{}, I<4>{}, F_{});
+    if constexpr (DW <= 128)
+      if (groups > 1) return go(I<2>{}, I<4>{}, F_{});
     if (splits > 1) return waves == 1 ? go(I<1>{}, I<1>{}, T_{}) : go(I<1>{}, I<4>{}, T_{});
     return waves == 1 ? go(I<1>{}, I<1>{}, F_{}) : go(I<1>{}, I<4>{}, F_{});
   });

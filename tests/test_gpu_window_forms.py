@@ -87,6 +87,26 @@ def test_two_groups_at_their_edges(dh):
         assert torch.isfinite(got["ctx"][1:]).all()
 
 
+# Head widths above 128 (bf16): whole workgroups of rows, a wavefront's rows, cut and whole streams, sinks in parts, tokens, infinities where nobody looks.
+@pytest.mark.parametrize("dh", [136, 192, 256])
+@pytest.mark.parametrize("B,Sq,Sk,H,Hkv,window,sinks", [(2, 500, 500, 4, 2, 130, 3), (1, 1300, 1300, 1, 1, 2000, 0), (3, 700, 700, 30, 30, 100, 70), (2, 9, 600, 4, 2, 300, 2),
+                                                        (5, 1, 900, 8, 2, 400, 4)])
+def test_wide_heads(B, Sq, Sk, H, Hkv, window, sinks, dh):
+    r = route(B, Sq, Sk, H, Hkv, dh, "bf16", window, sinks)
+    assert (r.form, r.waves, r.fwd_groups, r.dq_groups) == (fax.FAX_ATTENTION_EDGE, 4 if Sq > 32 else 1, 1, 1), forms(r)
+    if H == 1 or Sq == 1:
+        assert r.fwd_splits > 1 and r.dq_splits > 1, forms(r)
+    if H == 30:
+        assert r.fwd_splits == 1 and r.dq_splits == 1 and r.key_splits == 1, forms(r)
+    q, k, v, d = make(B, Sq, Sk, H, Hkv, dh, "bf16")
+    k_len = (Sk - 60 * torch.arange(B)).to(torch.int32)
+    q_pos = k_len - Sq
+    ref = orc.window_attention(q.double(), k.double(), v.double(), window, sinks, q_pos, k_len, d.double(), TD["bf16"])
+    for b in range(B):
+        k[b, k_len[b]:], v[b, k_len[b]:] = math.inf, math.nan
+    check(run(*(t.to(DEV) for t in (q, k, v, d)), window, sinks, q_pos, k_len), ref)
+
+
 @pytest.mark.parametrize("dtype", ["bf16", "f32"])
 def test_sinks_alone_are_cut(dtype):
     B, S, H, window, sinks = 6, 1400, 8, 20, 5
@@ -105,7 +125,7 @@ def test_single_tokens_of_many_caches(dh, dtype):
 
 
 def test_scalar_kernels_take_the_rest():
-    for dh, dtype in ((33, "bf16"), (136, "bf16"), (256, "f32"), (6, "f32")):
+    for dh, dtype in ((33, "bf16"), (132, "bf16"), (256, "f32"), (6, "f32")):
         assert route(1, 50, 50, 2, 2, dh, dtype, 10, 0).form == fax.FAX_ATTENTION_SCALAR
         both(1, 50, 50, 2, 2, dh, dtype, 10, 2)
 
