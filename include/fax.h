@@ -455,7 +455,7 @@ int fax_embedding_bwd(int dtype, int N, int V, int D, const int32_t* tokens, con
  *   2^30 - Sq above that.  Rows of k and v from k_len on are not used, whatever they hold, and get zeros in dk and dv.
  * Sizes up to B Sq H = 2^27, B Sk Hkv = 2^27, B Hkv = 2^21, dh <= 256, window >= 1, sinks >= 0; H a multiple of Hkv.
  * q, k, v, ctx and their gradients may start at any element (not the 16-byte alignment of the other calls): rows that start on 16 bytes take the
- *   matrix cores where the head width is a multiple of 16 bytes and at most 128 (fax_window_attention_route tells), others scalar kernels.
+ *   matrix cores where the head width is a multiple of 16 bytes and at most 256, of fp32 128 (fax_window_attention_route tells), others scalar kernels.
  * lse may be NULL in the forward pass (inference).  Backward: ctx, lse as the forward pass left them; dq, dk, dv are overwritten.
  * ws: fax_window_attention_workspace_bytes(), which covers both passes.  Nothing in it is kept from call to call.
  * No atomics: two calls on the same inputs give the same bits.
@@ -473,7 +473,8 @@ typedef struct FaxWindowDims {
  *   form         FAX_ATTENTION_*, as in FaxAttentionRoute.
  *   waves        bf16: wavefronts of a workgroup of the forward pass and dQ, 32 rows (queries of all heads of a key head) each: 4, or 1 for
  *                up to 32 rows.  fp32: 1, a tile of 32 rows.
- *   fwd_groups, dq_groups    bf16: such sets of wavefronts in a workgroup, which have the same rows and share the keys: 2 where workgroups are no more than CUs.
+ *   fwd_groups, dq_groups    bf16: such sets of wavefronts in a workgroup, which have the same rows and share the keys: 2 where workgroups
+ *                are no more than CUs, streams not cut and several tiles long, and the head width at most 128.
  *   fwd_splits, dq_splits    runs of keys that a row's forward pass and its dQ are cut into, which a second kernel joins (1: none).
  *   sink_splits, key_splits  runs of queries that dK and dV are cut into (1: none): of the sinks (and the keys that share a tile with them), which
  *                every later query sees, and of the other keys.
