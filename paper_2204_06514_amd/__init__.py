@@ -422,14 +422,15 @@ def window_dims(q, k, window, sinks=0, ctx=None):
 
 
 def _layouts(dims):
-    """(shape, strides) of q, kv and ctx as `dims` says, worked out once for as long as it says so."""
+    """(shape, strides, type) of q, kv and ctx as `dims` says, worked out once for as long as it says so."""
     raw, known = bytes(dims), getattr(dims, "_known", None)
     if known is None or known[0] != raw:
         found = {}
         for name, rows, heads in (("q", dims.Sq, dims.H), ("kv", dims.Sk, dims.Hkv), ("ctx", dims.Sq, dims.H)):
             f = getattr(dims, name)
             s = (f.batch, f.row, f.head)
-            found[name] = ((dims.B, rows, heads, dims.dh), (s if any(s) else (rows * heads * dims.dh, heads * dims.dh, dims.dh)) + (1,))
+            found[name] = ((dims.B, rows, heads, dims.dh), (s if any(s) else (rows * heads * dims.dh, heads * dims.dh, dims.dh)) + (1,),
+                           {FAX_F32: torch.float32, FAX_BF16: torch.bfloat16}.get(dims.dtype))
         known = dims._known = (raw, found)
     return known[1]
 
@@ -438,7 +439,8 @@ def _laid_out(t, layout):
     """Address of a tensor that is laid out like that (an address is taken as it is)."""
     if t is None or isinstance(t, int):
         return t
-    shape, strides = layout
+    shape, strides, dtype = layout
+    assert t.dtype is dtype, "a tensor of %s where dims say %s" % (t.dtype, dtype)
     assert t.shape == shape, "a tensor of %s where dims say %s" % (tuple(t.shape), shape)
     s = t.stride()
     assert s == strides or all(n == 1 or x == y for n, x, y in zip(shape, s, strides)), "strides %s where dims say %s" % (s, strides)

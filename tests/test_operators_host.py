@@ -185,3 +185,15 @@ def test_adamw_of_more_than_memory_holds():
     one = (fax.FaxAdamWTensor * 1)(fax.FaxAdamWTensor(A, A, A, A, None, None, None, (1 << 35) + 1, fax.FAX_F32, 1))
     hp = fax.FaxAdamW(1e-3, 0.9, 0.95, 1e-8, 0.1)
     refused(UNSUPPORTED, "elements", fax.fax_adamw_multi_step, fax.FAX_STATE_F32, (one, 1), hp, 1, 0, stream=0)
+
+
+def test_window_tensors_are_as_dims_say():
+    import torch
+    q, k = torch.zeros(1, 5, 2, 8), torch.zeros(1, 5, 2, 8)
+    d = fax.window_dims(q, k, 3)
+    call = lambda v, ctx=q: fax.fax_window_attention_fwd(d, q, k, v, None, None, ctx, None, A, 1 << 20, stream=0)  # noqa: E731
+    for v in (k.bfloat16(), k[:, :4], torch.zeros(1, 5, 2, 16)[..., :8], k.permute(0, 1, 3, 2)):
+        with pytest.raises(AssertionError):
+            call(v)
+    with pytest.raises(AssertionError):
+        call(k, ctx=q.bfloat16())
