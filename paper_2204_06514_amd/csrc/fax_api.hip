@@ -1276,7 +1276,7 @@ int fax_adamw_multi_step(int state, int count, const FaxAdamWTensor* tensors, co
     }
     if (t.lowp && misaligned(t.lowp)) { set_error("tensors[%d].lowp is not 16-byte aligned", i); return FAX_ERR_INVALID_ARG; }
     if (t.grad_dtype != FAX_F32 && t.grad_dtype != FAX_BF16) { set_error("tensors[%d].grad_dtype must be FAX_F32 or FAX_BF16", i); return FAX_ERR_INVALID_ARG; }
-    if (t.n > (size_t)1 << 35) { set_error("tensors[%d]: %zu elements", i, t.n); return FAX_ERR_UNSUPPORTED; }
+    if (t.n > (size_t)1 << 33) { set_error("tensors[%d]: %zu elements", i, t.n); return FAX_ERR_UNSUPPORTED; }
     if (state == FAX_STATE_E4M3) {
       if (!t.m_scale || !t.v_scale) { set_error("tensors[%d]: m_scale or v_scale is NULL", i); return FAX_ERR_INVALID_ARG; }
       if ((reinterpret_cast<uintptr_t>(t.m_scale) | reinterpret_cast<uintptr_t>(t.v_scale)) & 3) {

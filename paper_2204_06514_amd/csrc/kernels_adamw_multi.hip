@@ -1,16 +1,18 @@
 // AdamW over many tensors in one launch, moments of 32 bits or of 8.
 //
-// Memory bound, one pass: 28 to 30 bytes an element with moments of 32 bits, 16 to 18 with moments of 8.  A workgroup has 4096
-// consecutive elements of one tensor; which, it looks up in the table that comes with the launch's arguments (MULTI_BATCH tensors: the
-// arguments of a launch are 4 KB).
-// Measured: the 148 tensors of a 12-layer, 768-wide model (125 M elements, fp32 gradients, bf16 copies) 727 us with moments of 32 bits (3.76 GB, 5.2 TB/s)
-// and 446 us with moments of 8 (2.26 GB, 5.05 TB/s); a large copy on the same card moves 4.7 to 5.0 TB/s.
+// Memory bound, one pass: 28 to 30 bytes an element with moments of 32 bits, 16 to 18 with moments of 8.  A workgroup has 1024
+// consecutive elements of one tensor, a wave a block that shares a scale; which tensor, it looks up in the table that comes with the launch's arguments
+// (MULTI_BATCH tensors: the arguments of a launch are 4 KB).  (4096 elements, four blocks to a wave one after another | 1024, us: 8 tensors of 50000, 8-bit 10.6 | 7.5;
+// of 500000 19.5 | 17.0, 32-bit 18.9 | 18.5; of 2 million 56.6 | 52.9, 68.8 | 64.7; of 8 million 216 | 217, 344 | 335.)
+// Measured: the 148 tensors of a 12-layer, 768-wide model (125 M elements, fp32 gradients, bf16 copies) 685 us with moments of 32 bits (3.76 GB, 5.5 TB/s)
+// and 444 us with moments of 8 (2.26 GB, 5.1 TB/s); a large copy on the same card moves 4.7 to 5.0 TB/s.
 #include "adamw.h"
 
 namespace fax {
 
 static constexpr int MULTI_BATCH = 48;
 static constexpr int BLOCK = 256;              // elements that share a scale: a wave's, four to a lane
+static constexpr int MULTI_CHUNK = 4 * BLOCK;  // elements of a workgroup
 static constexpr float E4M3_MAX = 448.f;
 static constexpr float M_FLOOR = 7.888609052e-31f;  // 2^-100: below, 448 / maximum would leave fp32
 static constexpr uint32_t HASH_C = 0x9E3779B1u, HASH_D = 0x2545F491u;
@@ -147,66 +149,61 @@ __global__ __launch_bounds__(256) void adamw_table_kernel(MultiTable b, AdamScal
   const int k = entry_of(b, blockIdx.x);
   const MultiEntry& e = b.t[k];
   const size_t n = e.n;
-  const size_t start = (size_t)(blockIdx.x - b.first[k]) * ADAM_CHUNK;
   if (!e.decay) a.decay = 1.f;
   const int lane = threadIdx.x & 63, wave = threadIdx.x >> 6;
+  const size_t block = (size_t)(blockIdx.x - b.first[k]) * MULTI_CHUNK + wave * BLOCK, i = block + lane * 4;
+  if (block >= n) return;
+  float4 p = load4(e.p, i, n);
+  const float4 g = e.g_bf16 ? load4((const bf16_t*)e.g, i, n) : load4((const float*)e.g, i, n);
+  if constexpr (!LOW8) {
+    float4 m = load4((const float*)e.m, i, n), v = load4((const float*)e.v, i, n);
+    update(g.x, p.x, m.x, v.x, a);
+    update(g.y, p.y, m.y, v.y, a);
+    update(g.z, p.z, m.z, v.z, a);
+    update(g.w, p.w, m.w, v.w, a);
+    store4((float*)e.m, i, n, m);
+    store4((float*)e.v, i, n, v);
+  } else {
+    const size_t at = block / BLOCK;
+    const float ms = e.m_scale[at], vs = e.v_scale[at];
+    float m[4], v[4];
+    unpack4(load4((const uint8_t*)e.m, i, n), m);
+    unpack4(load4((const uint8_t*)e.v, i, n), v);
+    const float gs[4] = {g.x, g.y, g.z, g.w};
+    float ps[4] = {p.x, p.y, p.z, p.w};
+    float m_top = 0.f, v_top = 0.f;
 #pragma unroll
-  for (int r = 0; r < ADAM_CHUNK / 1024; r++) {
-    const size_t block = start + (size_t)(wave * (ADAM_CHUNK / 1024) + r) * BLOCK;  // a wave's blocks are neighbours
-    const size_t i = block + lane * 4;
-    if (block >= n) return;
-    float4 p = load4(e.p, i, n);
-    const float4 g = e.g_bf16 ? load4((const bf16_t*)e.g, i, n) : load4((const float*)e.g, i, n);
-    if constexpr (!LOW8) {
-      float4 m = load4((const float*)e.m, i, n), v = load4((const float*)e.v, i, n);
-      update(g.x, p.x, m.x, v.x, a);
-      update(g.y, p.y, m.y, v.y, a);
-      update(g.z, p.z, m.z, v.z, a);
-      update(g.w, p.w, m.w, v.w, a);
-      store4((float*)e.m, i, n, m);
-      store4((float*)e.v, i, n, v);
-    } else {
-      const size_t at = block / BLOCK;
-      const float ms = e.m_scale[at], vs = e.v_scale[at];
-      float m[4], v[4];
-      unpack4(load4((const uint8_t*)e.m, i, n), m);
-      unpack4(load4((const uint8_t*)e.v, i, n), v);
-      const float gs[4] = {g.x, g.y, g.z, g.w};
-      float ps[4] = {p.x, p.y, p.z, p.w};
-      float m_top = 0.f, v_top = 0.f;
-#pragma unroll
-      for (int q = 0; q < 4; q++) {
-        m[q] *= ms;
-        v[q] *= vs;
-        v[q] *= v[q];
-        update(gs[q], ps[q], m[q], v[q], a);
-        v[q] = sqrtf(v[q]);
-        if (finite(m[q])) m_top = fmaxf(m_top, fabsf(m[q]));
-        if (finite(v[q])) v_top = fmaxf(v_top, v[q]);
-      }
-      p = make_float4(ps[0], ps[1], ps[2], ps[3]);
-      m_top = wave_max(m_top);
-      v_top = wave_max(v_top);
-      if (m_top < M_FLOOR) m_top = 0.f;
-      const float m_inv = m_top > 0.f ? 1.f / m_top * E4M3_MAX : 0.f, v_inv = v_top > 0.f ? 1.f / v_top * E4M3_MAX : 0.f;
-#pragma unroll
-      for (int q = 0; q < 4; q++) {
-        const float nan = __builtin_nanf("");
-        m[q] = finite(m[q]) ? fminf(fmaxf(m[q] * m_inv, -E4M3_MAX), E4M3_MAX) : nan;
-        const uint32_t bits = hash32((uint32_t)(i + q) * HASH_C + e.key) >> 12;
-        const float x = v[q];
-        v[q] = !finite(x) ? nan : x > 0.f ? fmaxf(round_random(x * v_inv, bits), 0.001953125f) : 0.f;
-      }
-      store4((uint8_t*)e.m, i, n, pack4(m));
-      store4((uint8_t*)e.v, i, n, pack4(v));
-      if (lane == 0) {
-        e.m_scale[at] = m_top * (1.f / E4M3_MAX);
-        e.v_scale[at] = v_top * (1.f / E4M3_MAX);
-      }
+    for (int q = 0; q < 4; q++) {
+      m[q] *= ms;
+      v[q] *= vs;
+      v[q] *= v[q];
+      update(gs[q], ps[q], m[q], v[q], a);
+      v[q] = sqrtf(v[q]);
+      if (finite(m[q])) m_top = fmaxf(m_top, fabsf(m[q]));
+      if (finite(v[q])) v_top = fmaxf(v_top, v[q]);
     }
-    store4(e.p, i, n, p);
-    if (e.lowp) store4(e.lowp, i, n, p);
+    p = make_float4(ps[0], ps[1], ps[2], ps[3]);
+    m_top = wave_max(m_top);
+    v_top = wave_max(v_top);
+    if (m_top < M_FLOOR) m_top = 0.f;
+    const float m_inv = m_top > 0.f ? 1.f / m_top * E4M3_MAX : 0.f, v_inv = v_top > 0.f ? 1.f / v_top * E4M3_MAX : 0.f;
+#pragma unroll
+    for (int q = 0; q < 4; q++) {
+      const float nan = __builtin_nanf("");
+      m[q] = finite(m[q]) ? fminf(fmaxf(m[q] * m_inv, -E4M3_MAX), E4M3_MAX) : nan;
+      const uint32_t bits = hash32((uint32_t)(i + q) * HASH_C + e.key) >> 12;
+      const float x = v[q];
+      v[q] = !finite(x) ? nan : x > 0.f ? fmaxf(round_random(x * v_inv, bits), 0.001953125f) : 0.f;
+    }
+    store4((uint8_t*)e.m, i, n, pack4(m));
+    store4((uint8_t*)e.v, i, n, pack4(v));
+    if (lane == 0) {
+      e.m_scale[at] = m_top * (1.f / E4M3_MAX);
+      e.v_scale[at] = v_top * (1.f / E4M3_MAX);
+    }
   }
+  store4(e.p, i, n, p);
+  if (e.lowp) store4(e.lowp, i, n, p);
 }
 
 int adamw_multi(int state, int count, const FaxAdamWTensor* tensors, const FaxAdamW& hp, int step, uint32_t seed, hipStream_t s) {
@@ -229,7 +226,7 @@ int adamw_multi(int state, int count, const FaxAdamWTensor* tensors, const FaxAd
   for (int t = 0; t < count; t++) {
     const FaxAdamWTensor& x = tensors[t];
     if (x.n == 0) continue;
-    const size_t chunks = (x.n + ADAM_CHUNK - 1) / ADAM_CHUNK;
+    const size_t chunks = (x.n + MULTI_CHUNK - 1) / MULTI_CHUNK;
     if (b.count == MULTI_BATCH || b.first[b.count] + chunks > 0xffffffu) FAX_TRY(flush());  // (fewer than 2^32 threads)
     MultiEntry& e = b.t[b.count];
     e.p = (float*)x.master; e.m = x.m; e.v = x.v; e.g = x.grad; e.lowp = (bf16_t*)x.lowp; e.n = x.n;
