@@ -17,7 +17,7 @@ LIB = os.path.join(HERE, "libfax.so")
 
 SOURCES = ["fax_api.hip", "kernels_norm.hip", "kernels_gemm_simt.hip", "kernels_gemm_f32.hip", "kernels_gemm_mfma.hip", "kernels_gemm_edge.hip", "kernels_gemm_deep.hip", "kernels_gemm_group.hip", "kernels_gemm_lse.hip",
            "kernels_attn_simt.hip", "kernels_attn_f32.hip", "kernels_attn_mfma.hip", "kernels_attn_dkv16.hip", "kernels_loss_opt.hip", "kernels_adamw_multi.hip",
-           "kernels_embedding.hip", "kernels_window.hip", "kernels_window_mfma.hip", "kernels_window_dkv.hip", "kernels_window_f32.hip",
+           "kernels_embedding.hip", "kernels_window.hip", "kernels_window_mfma.hip", "kernels_window_wide.hip", "kernels_window_dkv.hip", "kernels_window_f32.hip",
            "analyze.hip", "probes.hip"]
 
 FLAGS = ["--offload-arch=gfx950", "-O3", "-std=c++17", "-fPIC", "-munsafe-fp-atomics",

@@ -31,6 +31,7 @@ struct WindowPlan {
   size_t delta, part_o, part_ml, part_dq, part_ds, parts, total;
 };
 int window_fwd_mfma(const WindowArgs& a, int waves, int groups, int splits, float* part_o, void* part_ml, hipStream_t s);
+int window_dq_wide(const WindowArgs& a, int waves, int splits, float* part_dq, float* part_ds, hipStream_t s);  // head widths above 128
 int window_dq_mfma(const WindowArgs& a, int waves, int groups, int splits, float* part_dq, float* part_ds, hipStream_t s);
 static constexpr int WINDOW_DKV_KEYS = 64;  // keys of a workgroup
 int window_dkv_mfma(const WindowArgs& a, const WindowPlan& p, float* parts, hipStream_t s);

@@ -6,7 +6,7 @@
 // large bf16 product of the same card 1211 to 1334 TFLOP/s.  8 x 2048 positions, 12 heads of 64, window 512: 59, 89 and 95 us: at width 64 there is
 // half the matrix work to a score, and the softmax's instructions and waits are the rest.  Single tokens, 8 sequences of 32 heads on 8 of 128, window 4096: 29 us
 // for the 134 MB of keys and values (4.6 TB/s) and 5 us for the join.
-// The scalar kernels are for the sizes that nothing else takes: 2048 positions, 8 heads of 256, window 512: 7.9 ms forward, 32 ms backward (1 TFLOP/s); on the matrix cores 35 and 131 us.
+// The scalar kernels are for the sizes that nothing else takes: 2048 positions, 8 heads of 256, window 512: 7.9 ms forward, 32 ms backward (1 TFLOP/s); on the matrix cores 35 and 88 us.
 #include <initializer_list>
 
 #include "window_tiles.h"
@@ -213,8 +213,8 @@ static int cut_stream(double blocks, long long tiles, const StreamCost& c, doubl
 // Head width 256, by parts again:
 //   forward  tokens over 4096 keys, 16 heads on 4: one  190  4: 72  8: 43  16: 28  32: 23  64: 21;  four  190  73  44  31  40  57;  sixteen  190  76  83
 //            512 queries over them, window 2048 (64 workgroups)  74  2: 68  4: 51  8: 65;  2048 of 8 on 8, 512 (128)  34  43  57
-//   backward, by parts of dQ's streams  2048 of 4 on 2, all (64)  285  198  156  184;  2048 of 8 on 8, 512 (128)  131  116  150;  two, 8 on 4 (256)  153  203
-//             by those of dK and dV     the same three  260  190  155  167;  131  159  187;  153  180  218
+//   backward, by parts of dQ's streams  2048 of 4 on 2, all (64)  177  134  115  132;  2048 of 8 on 8, 512 (128)  88  84  105;  two, 8 on 4 (256)  112  142
+//             by those of dK and dV     the same three  218  149  114  125;  87  115  144;  111  137  164
 static WindowPlan window_plan(const FaxWindowDims& d) {
   WindowPlan p = {};
   p.form = FAX_ATTENTION_SCALAR;

@@ -8,8 +8,7 @@
 //   * Groups (G = 2): two groups of four wavefronts have the same rows and take every other tile, each with LDS buffers of its own, and add up through LDS:
 //     where there is a workgroup to a CU or less, whose four wavefronts would be alone on their SIMDs.
 //   * Head widths above 128 are computed at 256: accumulators and fragments take 360 to 512 registers and two stages of tiles 128 KB, one workgroup to
-//     a CU.  (dQ does not quite fit: 512 bytes a lane go to scratch, a quarter of the accesses between products.)  2 x 4096 positions, 16 heads on 4 of 256, window 1024,
-//     sinks 4: forward 177 us (680 TFLOP/s), backward 938 us (320).
+//     a CU.  2 x 4096 positions, 16 heads on 4 of 256, window 1024, sinks 4: forward 178 us (680 TFLOP/s), backward 655 us (460).
 //   * Rows of a tile from the last key on are loads of the last key (never a read out of bounds, nothing left in LDS that was not loaded).
 #pragma once
 #include "attn_dkv16.h"

@@ -13,3 +13,10 @@ def test_window_tile_loads_are_waited_for(tmp_path):
         n, bad = scan(text.replace("window_", "attn_window_"), r"_ZN3fax\d+attn_window_\w+")  # none allowed in flight
         assert n >= kernels, (name, n)
         assert not bad, {k: v[:3] for k, v in bad.items()}
+
+
+def test_wide_tile_loads_are_waited_for(tmp_path):
+    text = _assembly(tmp_path, os.path.join(CSRC, "kernels_window_wide.hip"), ())
+    n, bad = scan(text.replace("window_", "attn_window_"), r"_ZN3fax\d+attn_window_\w+")
+    assert n >= 4, n
+    assert not bad, {k: v[:3] for k, v in bad.items()}
